@@ -256,6 +256,131 @@ int spb_aggregate_update(spb_model* m, int32_t n_workers, const int32_t* depths,
                          void* const* velocity, float lr, float momentum, float weight_decay, int32_t scale_lr,
                          void* stream);
 
+/* ---- Heads: layer norm and rotary positions of query and key rows ---------------------------------------------
+ * Between the projection and the attention of an encoder layer: each head's row of a token is normed over its
+ * elements, turned by the token's positions, or both, in one pass.
+ *   norm      n = gamma * (x - mean) / sqrt(var + eps) + beta over the head_dim elements of the row
+ *   rotation  pair j of the row turns by t = freq[j] * (the token's position on axis[j]), a whole number:
+ *             (u, v) -> (u cos t - v sin t, u sin t + v cos t).  Pair j is elements j and j + pairs, or, interleaved,
+ *             2j and 2j + 1; elements from 2 * pairs on are not turned.
+ * Positions on one to four axes (time, height, width, ...) may be any int32; angles are formed in float64, everything
+ * else is float32, rounded once to the storage type.  These calls need no model: they enqueue on `stream`, allocate
+ * nothing and may be captured into a HIP graph. */
+#define SPB_MAX_HEAD_DIM 256
+#define SPB_MAX_PAIRS 128
+#define SPB_MAX_AXES 4
+
+typedef struct spb_rotary {
+  int32_t pairs;               /* turned pairs of a head, 0..head_dim / 2 */
+  int32_t interleaved;         /* which elements make pair j, see above */
+  int32_t axes;                /* 1..SPB_MAX_AXES */
+  int32_t reserved;            /* 0 */
+  int32_t axis[SPB_MAX_PAIRS]; /* axis of pair j, in [0, axes) */
+  double freq[SPB_MAX_PAIRS];  /* radians per unit of position, finite */
+} spb_rotary;
+
+typedef struct spb_heads_desc {
+  int32_t dtype;               /* SPB_DTYPE_F32 or SPB_DTYPE_BF16: x, y, dy, dx, gamma, beta */
+  int32_t batch, seq;          /* tokens: batch * seq, at most 2^31 - 1; either may be 0 */
+  int32_t heads_q, heads_k;    /* the first heads_q >= 1 heads take row 0 of gamma and beta, the heads_k >= 0 behind them row 1 */
+  int32_t head_dim;            /* 1..SPB_MAX_HEAD_DIM */
+  int32_t norm;                /* non-zero: with norm */
+  float eps;                   /* > 0 with norm */
+  int64_t x_stride[3];         /* elements from one sequence, token, head to the next; the elements of a head are contiguous.  Inputs may */
+  int64_t y_stride[3];         /*   repeat (stride 0); rows of y and dx may not overlap.  y_stride is y's in the forward call and dy's in */
+  int64_t dx_stride[3];        /*   the backward call; dx_stride is read by the backward call only */
+  spb_rotary rotary;           /* pairs = 0: no rotation (the rest is not read) */
+} spb_heads_desc;
+
+/* Fills a rotary description: sections[a] pairs for axis a, in order.  Pair j of the P = sum of sections has frequency base^(-j / P), or, with
+ * own_ladder, the i-th pair of axis a base^(-i / sections[a]).  Host-only.
+ * Errors: INVALID_ARG (null, axes outside 1..SPB_MAX_AXES, a negative section, no or more than SPB_MAX_PAIRS pairs, base not positive and finite). */
+int spb_rotary_sections(spb_rotary* out, int32_t axes, const int32_t* sections, double base, int32_t own_ladder, int32_t interleaved);
+
+/* y = rotation(norm(x)).
+ *   x, y   device, [batch][seq][heads_q + heads_k][head_dim] with the strides of the description; y may be x, with the same strides
+ *   pos    device, int32: the position of token s of sequence b on axis a is pos[a * pos_axis_stride + b * pos_batch_stride + s] (batch
+ *          stride 0: the same for all sequences); NULL without rotation
+ *   gamma  device, [heads_k ? 2 : 1][head_dim] with norm, NULL without; beta the same, or NULL for none
+ * Errors: INVALID_ARG (also: neither norm nor rotation), HIP. */
+int spb_heads_forward(const spb_heads_desc* d, const void* x, void* y, const int32_t* pos, int64_t pos_axis_stride, int64_t pos_batch_stride,
+                      const void* gamma, const void* beta, void* stream);
+
+/* Bytes of workspace of spb_heads_backward: 0 without norm. */
+int spb_heads_workspace_size(const spb_heads_desc* d, size_t* bytes);
+
+/* dx and, with norm, the gradients of gamma and beta, from the forward call's x and the gradient dy at its y.
+ *   x              the forward call's input (not read without norm, may be NULL then)
+ *   dy, dx         dx may be dy or x, with the same strides
+ *   gamma          the forward call's
+ *   dgamma, dbeta  device, float32, gamma's shape, overwritten, summed over all tokens and the heads of a row in a fixed order (the same bits on every run)
+ *   workspace      device, 256-byte aligned, >= spb_heads_workspace_size bytes, until the call has completed on the device; NULL without norm
+ * Errors: INVALID_ARG, WORKSPACE, HIP. */
+int spb_heads_backward(const spb_heads_desc* d, const void* x, const void* dy, void* dx, const int32_t* pos, int64_t pos_axis_stride,
+                       int64_t pos_batch_stride, const void* gamma, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gives every layer of an encoder the above between its query/key projection and its attention; to be called before its parameters are
+ * bound and its workspace sized (sizes grow with norm).  An encoder is created without.
+ *   rotary  copied; NULL: no rotation.  2 * pairs <= hidden / heads
+ *   pos     as above, for [batch][seq] tokens; read by every later forward and backward pass, so it stays alive and unchanged from a forward
+ *           pass to the end of the matching backward pass
+ *   norm    non-zero: parameters layer<i>.attn.qknorm.weight and .bias of shape [2, hidden / heads] (row 0 queries, row 1 keys) follow each
+ *           layer's attn.qkv.bias in the parameter list, with eps > 0
+ * Without either the encoder is as created.  The learned position table stays; a caller who wants rotary positions alone keeps it at zero.
+ * Errors: INVALID_ARG, STATE (parameters or gradients are bound), UNSUPPORTED (not an encoder). */
+int spb_encoder_heads(spb_model* m, const spb_rotary* rotary, const int32_t* pos, int64_t pos_axis_stride, int64_t pos_batch_stride, int32_t norm,
+                      float eps);
+
+/* ---- Orthogonalised updates ----------------------------------------------------------------------------------
+ * One optimiser step over the averaged gradients of up to SPB_MAX_WORKERS workers.  g = mean of the tensor's gradients, rate = lr * rate_scale.
+ *   matrices (blocks >= 1; each of the `blocks` equal groups of rows is one matrix of its own, e.g. 3 for stacked query, key and value weights):
+ *       m = momentum m + g;  u = g + momentum m (nesterov) or m;  X = u / (|u| + ns_eps), |u| the root of the sum of squares;
+ *       ns_steps times, with the shorter side first:  A = X X^T;  X = 3.4445 X + (-4.7750 A + 2.0315 A A) X;
+ *       w = w (1 - rate weight_decay) - rate rms sqrt(longer side) X
+ *     (the quintic Newton-Schulz step, which moves every singular value towards 1; a full-rank update then has entries of root mean square rate * rms)
+ *   others (blocks = 0), AdamW:
+ *       m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2;
+ *       w = w (1 - rate weight_decay) - rate (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + adam_eps)
+ * m and v are float32.  A bfloat16 parameter is rounded to nearest-even after the float32 update.  The products accumulate in float32; between them X is
+ * held to 11 bits for bfloat16 parameters and to 22 bits for float32 ones. */
+typedef struct spb_muon_tensor {
+  void* w;                     /* device, [rows, cols] dense, updated in place */
+  float* m;                    /* device, the same shape: momentum, or AdamW's first moment; updated in place */
+  float* v;                    /* device, the same shape: AdamW's second moment; NULL for matrices */
+  const float* const* grads;   /* HOST array of `count` device pointers, each the same shape */
+  int64_t rows, cols;          /* a tensor of more dimensions: rows = the first, cols = the product of the rest */
+  double rate_scale;           /* >= 0 */
+  int32_t count;               /* 1..SPB_MAX_WORKERS */
+  int32_t dtype;               /* of w */
+  int32_t blocks;              /* 0: AdamW; >= 1: matrices of rows / blocks by cols, each side at most SPB_MAX_MATRIX_SIDE */
+  int32_t reserved;            /* 0 */
+} spb_muon_tensor;
+#define SPB_MAX_MATRIX_SIDE 65536
+
+typedef struct spb_muon_config {
+  double lr, rms, momentum, ns_eps;
+  double beta1, beta2, adam_eps, weight_decay;
+  int64_t step;                /* >= 1: how many steps AdamW's moments have seen, this one included.  (A captured call replays with this value.) */
+  int32_t nesterov, ns_steps;  /* ns_steps in 1..16 */
+} spb_muon_config;
+
+/* Bytes of workspace of a step over these tensors: 0 if none is a matrix.  Device pointers are not looked at. */
+int spb_muon_workspace_size(const spb_muon_tensor* tensors, int32_t n, size_t* bytes);
+
+/* One step over n tensors, enqueued on `stream`; needs no model, allocates nothing and may be captured into a HIP graph.
+ *   workspace  device, 256-byte aligned, until the call has completed on the device; NULL if the size is 0
+ * Errors: INVALID_ARG (null or misaligned pointers, the same w twice, values outside their ranges), WORKSPACE, HIP. */
+int spb_muon_step(const spb_muon_tensor* tensors, int32_t n, const spb_muon_config* config, void* workspace, size_t workspace_bytes, void* stream);
+
+/* spb_aggregate_update with the step above in place of SGD: same workers, depths, averaging and rate scaling.
+ *   blocks         host array [n_params]: 0 AdamW, >= 1 matrices, as in spb_muon_tensor (rows = a parameter's first dimension)
+ *   first, second  host arrays [n_params] of device pointers, float32, the parameter's shape: m and v; second may hold NULL for matrices
+ * A parameter no worker contributed to is left untouched, moments included.  The size covers any depths.
+ * Errors: as spb_aggregate_update, WORKSPACE. */
+int spb_aggregate_muon_workspace_size(const spb_model* m, const int32_t* blocks, size_t* bytes);
+int spb_aggregate_muon(spb_model* m, int32_t n_workers, const int32_t* depths, void* const* worker_grads, const int32_t* blocks, void* const* first,
+                       void* const* second, const spb_muon_config* config, int32_t scale_lr, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Kernel timing.  When enabled, every kernel the model enqueues is bracketed by two HIP events on
  * the launch stream.  spb_read_kernel_timing waits for the recorded events, adds them up per kernel
  * class into out (host array of cap records; n_out receives the count) and clears the record.

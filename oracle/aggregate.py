@@ -48,3 +48,49 @@ def aggregate_update(param_units: dict, n_units: int, params: dict, velocity: di
         new_v[name] = v
         new_w[name] = q(w - rate * v)
     return new_w, new_v
+
+
+def orthogonalise(u, steps: int = 5, eps: float = 1e-7):
+    """Newton-Schulz: X = u / (|u|_F + eps), then `steps` times X <- p(X), the odd quintic p(s) = 3.4445 s - 4.7750 s^3 + 2.0315 s^5 applied to the
+    singular values, which lets those of a full-rank matrix end near 1."""
+    x = np.asarray(u, dtype=np.float64)
+    x = x / (np.sqrt((x * x).sum()) + eps)
+    for _ in range(steps):
+        gram = x @ x.T if x.shape[0] <= x.shape[1] else x.T @ x
+        poly = 3.4445 * np.eye(len(gram)) - 4.7750 * gram + 2.0315 * gram @ gram
+        x = poly @ x if x.shape[0] <= x.shape[1] else x @ poly
+    return x
+
+
+def muon_step(w, m, v, grads, blocks: int, rate: float, hyper: dict):
+    """One optimiser step of one parameter from its contributors' gradients: (w, m, v), all float64.  blocks >= 1: that many equal groups of rows
+    are matrices, whose momentum is orthogonalised; 0: AdamW."""
+    w, m = np.asarray(w, dtype=np.float64), np.asarray(m, dtype=np.float64)
+    g = sum(np.asarray(x, dtype=np.float64) for x in grads) / len(grads)
+    keep = 1.0 - rate * hyper["weight_decay"]
+    if blocks == 0:
+        m = hyper["beta1"] * m + (1.0 - hyper["beta1"]) * g
+        v = hyper["beta2"] * np.asarray(v, dtype=np.float64) + (1.0 - hyper["beta2"]) * g * g
+        step = (m / (1.0 - hyper["beta1"] ** hyper["step"])) / (np.sqrt(v / (1.0 - hyper["beta2"] ** hyper["step"])) + hyper["adam_eps"])
+        return keep * w - rate * step, m, v
+    m = hyper["momentum"] * m + g
+    u = (g + hyper["momentum"] * m if hyper["nesterov"] else m).reshape(blocks, w.shape[0] // blocks, -1)
+    x = np.stack([orthogonalise(b, hyper["ns_steps"], hyper["ns_eps"]) for b in u])
+    return keep * w - rate * hyper["rms"] * math.sqrt(max(u.shape[1:])) * x.reshape(w.shape), m, None
+
+
+def aggregate_muon(param_units: dict, n_units: int, params: dict, first: dict, second: dict, worker_grads: list, depths, blocks: dict, hyper: dict,
+                   scale_lr: bool, q=lambda a: a):
+    """aggregate_update with muon_step in place of SGD.  Returns (new params, new first moments, new second moments)."""
+    out = {}, {}, {}
+    for name, unit in param_units.items():
+        who = contributors(unit, n_units, depths)
+        if not who:
+            new = tuple(None if t is None else np.asarray(t, dtype=np.float64) for t in (params[name], first[name], second.get(name)))
+        else:
+            rate = hyper["lr"] * len(who) / len(depths) if scale_lr else hyper["lr"]
+            new = muon_step(params[name], first[name], second.get(name), [worker_grads[j][name] for j in who], blocks[name], rate, hyper)
+            new = (q(new[0]),) + new[1:]
+        for d, t in zip(out, new):
+            d[name] = t
+    return out

@@ -90,6 +90,43 @@ def softmax_rows(s):
     return e / e.sum(axis=-1, keepdims=True)
 
 
+def head_norm_fwd(x, gamma, beta, eps):
+    """Layer norm of each head's row: x [tokens, heads, d], gamma and beta [heads, d].  Returns y and what the backward pass needs."""
+    off = x - x.mean(axis=-1, keepdims=True)
+    rstd = 1.0 / np.sqrt((off * off).mean(axis=-1, keepdims=True) + eps)
+    return gamma * (off * rstd) + beta, (off * rstd, rstd)
+
+
+def head_norm_bwd(dy, gamma, cache):
+    """dx, and per head the gradients of gamma and beta."""
+    xhat, rstd = cache
+    g = dy * gamma
+    dx = (g - g.mean(axis=-1, keepdims=True) - xhat * (g * xhat).mean(axis=-1, keepdims=True)) * rstd
+    return dx, (dy * xhat).sum(axis=0), dy.sum(axis=0)
+
+
+def rotary_angles(positions, sections, base=10000.0, own_ladder=False, interleaved=False):
+    """positions [axes, tokens] -> the angle of every pair [tokens, pairs]: pairs in sections, one axis after the other; the frequency of pair j of P is
+    base^(-j / P), or base^(-i / section) for the i-th pair of a section."""
+    total, cols, j = sum(sections), [], 0
+    for axis, count in enumerate(sections):
+        for i in range(count):
+            cols.append(np.asarray(positions[axis], dtype=np.float64) * base ** (-(i / count) if own_ladder else -(j / total)))
+            j += 1
+    return np.stack(cols, axis=-1)
+
+
+def rotate(x, angles, interleaved=False):
+    """Turns pair j of every row of x [tokens, heads, d] by angles [tokens, pairs]: elements (j, j + pairs), or (2j, 2j + 1)."""
+    p = angles.shape[-1]
+    lo, hi = (slice(0, 2 * p, 2), slice(1, 2 * p, 2)) if interleaved else (slice(0, p), slice(p, 2 * p))
+    c, s = np.cos(angles)[:, None, :], np.sin(angles)[:, None, :]
+    out = x.copy()
+    out[..., lo] = x[..., lo] * c - x[..., hi] * s
+    out[..., hi] = x[..., lo] * s + x[..., hi] * c
+    return out
+
+
 def split_heads(t, batch, seq, heads):
     """[batch * seq, heads * d] -> [batch, heads, seq, d]."""
     d = t.shape[1] // heads

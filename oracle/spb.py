@@ -123,16 +123,46 @@ class EncoderLayerUnit:
         self.pre = f"layer{index}."
         self.batch, self.seq, self.heads = cfg["batch"], cfg["seq"], cfg["heads"]
         self.d = cfg["hidden"] // cfg["heads"]
+        self.rotary, self.eps = cfg.get("rotary"), cfg.get("qk_norm")
+        norm = ("attn.qknorm.weight", "attn.qknorm.bias") if self.eps else ()
         self.param_names = [self.pre + n for n in (
-            "ln1.weight", "ln1.bias", "attn.qkv.weight", "attn.qkv.bias", "attn.out.weight", "attn.out.bias",
+            "ln1.weight", "ln1.bias", "attn.qkv.weight", "attn.qkv.bias", *norm, "attn.out.weight", "attn.out.bias",
             "ln2.weight", "ln2.bias", "ffn.w1.weight", "ffn.w1.bias", "ffn.w2.weight", "ffn.w2.bias")]
+
+    def heads_forward(self, qkv, P, q, batch):
+        """Query and key rows normed and turned by the tokens' positions, where the configuration says so."""
+        if not (self.rotary or self.eps):
+            return qkv
+        hidden = qkv.shape[1] // 3
+        x = qkv[:, :2 * hidden].reshape(-1, 2 * self.heads, self.d)
+        if self.eps:
+            self.row_weight = np.repeat(P("attn.qknorm.weight"), self.heads, axis=0)      # row 0 for the queries, row 1 for the keys
+            x, self.qk_cache = ops.head_norm_fwd(x, self.row_weight, np.repeat(P("attn.qknorm.bias"), self.heads, axis=0), self.eps)
+        if self.rotary:
+            pos = np.broadcast_to(np.asarray(batch["positions"]), (len(self.rotary["sections"]), self.batch, self.seq))
+            self.angles = ops.rotary_angles(pos.reshape(pos.shape[0], -1), **self.rotary)
+            x = ops.rotate(x, self.angles, self.rotary.get("interleaved", False))
+        return np.concatenate([q(x.reshape(-1, 2 * hidden)), qkv[:, 2 * hidden:]], axis=1)
+
+    def heads_backward(self, dqkv, q, g):
+        if not (self.rotary or self.eps):
+            return dqkv
+        hidden = dqkv.shape[1] // 3
+        d = dqkv[:, :2 * hidden].reshape(-1, 2 * self.heads, self.d)
+        if self.rotary:
+            d = ops.rotate(d, -self.angles, self.rotary.get("interleaved", False))
+        if self.eps:
+            d, scale, shift = ops.head_norm_bwd(d, self.row_weight, self.qk_cache)
+            g[self.pre + "attn.qknorm.weight"] = scale.reshape(2, self.heads, -1).sum(axis=1)
+            g[self.pre + "attn.qknorm.bias"] = shift.reshape(2, self.heads, -1).sum(axis=1)
+        return np.concatenate([q(d.reshape(-1, 2 * hidden)), dqkv[:, 2 * hidden:]], axis=1)
 
     def forward(self, x, p, q, batch):
         P = lambda n: p[self.pre + n]
         hidden = x.shape[1]
         u, self.ln1 = ops.layernorm_fwd(x, P("ln1.weight"), P("ln1.bias"))
         self.u = q(u)
-        self.qkv = q(ops.linear_fwd(self.u, P("attn.qkv.weight"), P("attn.qkv.bias")))
+        self.qkv = self.heads_forward(q(ops.linear_fwd(self.u, P("attn.qkv.weight"), P("attn.qkv.bias"))), P, q, batch)
         qh, kh, vh = (ops.split_heads(self.qkv[:, i * hidden:(i + 1) * hidden], self.batch, self.seq, self.heads) for i in range(3))
         scores = qh @ kh.transpose(0, 1, 3, 2) / np.sqrt(self.d)
         self.prob = q(ops.softmax_rows(scores))
@@ -166,7 +196,7 @@ class EncoderLayerUnit:
         ds = q(self.prob * (dprob - (dprob * self.prob).sum(axis=-1, keepdims=True)) / np.sqrt(self.d))
         dqh = ds @ kh
         dkh = ds.transpose(0, 1, 3, 2) @ qh
-        dqkv = q(np.concatenate([ops.merge_heads(t) for t in (dqh, dkh, dvh)], axis=1))
+        dqkv = self.heads_backward(q(np.concatenate([ops.merge_heads(t) for t in (dqh, dkh, dvh)], axis=1)), q, g)
         g[self.pre + "attn.qkv.weight"], g[self.pre + "attn.qkv.bias"], du = ops.linear_bwd(dqkv, self.u, P("attn.qkv.weight"), True)
         du = q(du)
         dx_ln, g[self.pre + "ln1.weight"], g[self.pre + "ln1.bias"] = ops.layernorm_bwd(du, P("ln1.weight"), self.ln1)

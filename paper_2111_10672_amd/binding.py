@@ -64,6 +64,30 @@ class spb_sched_task(C.Structure):
                 ("moved", C.c_int32), ("start", C.c_double), ("end", C.c_double), ("held_until", C.c_double)]
 
 
+SPB_MAX_HEAD_DIM, SPB_MAX_PAIRS, SPB_MAX_AXES, SPB_MAX_MATRIX_SIDE = 256, 128, 4, 65536
+
+
+class spb_rotary(C.Structure):
+    _fields_ = [("pairs", C.c_int32), ("interleaved", C.c_int32), ("axes", C.c_int32), ("reserved", C.c_int32),
+                ("axis", C.c_int32 * SPB_MAX_PAIRS), ("freq", C.c_double * SPB_MAX_PAIRS)]
+
+
+class spb_heads_desc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("seq", C.c_int32), ("heads_q", C.c_int32), ("heads_k", C.c_int32),
+                ("head_dim", C.c_int32), ("norm", C.c_int32), ("eps", C.c_float), ("x_stride", C.c_int64 * 3), ("y_stride", C.c_int64 * 3),
+                ("dx_stride", C.c_int64 * 3), ("rotary", spb_rotary)]
+
+
+class spb_muon_tensor(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("grads", C.POINTER(C.c_void_p)), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("rate_scale", C.c_double), ("count", C.c_int32), ("dtype", C.c_int32), ("blocks", C.c_int32), ("reserved", C.c_int32)]
+
+
+class spb_muon_config(C.Structure):
+    _fields_ = [("lr", C.c_double), ("rms", C.c_double), ("momentum", C.c_double), ("ns_eps", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
+                ("adam_eps", C.c_double), ("weight_decay", C.c_double), ("step", C.c_int64), ("nesterov", C.c_int32), ("ns_steps", C.c_int32)]
+
+
 _TASK = struct.Struct("<4i?7x3d")     # spb_sched_task; `moved` is 0 or 1, so its lowest byte says it
 assert _TASK.size == C.sizeof(spb_sched_task)
 
@@ -88,6 +112,17 @@ EXPORTS = {
     "spb_worker_depth": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_int32)]),
     "spb_aggregate_update": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                        C.c_float, C.c_float, C.c_float, C.c_int32, C.c_void_p]),
+    "spb_rotary_sections": (C.c_int, [C.POINTER(spb_rotary), C.c_int32, C.POINTER(C.c_int32), C.c_double, C.c_int32, C.c_int32]),
+    "spb_heads_forward": (C.c_int, [C.POINTER(spb_heads_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "spb_heads_workspace_size": (C.c_int, [C.POINTER(spb_heads_desc), C.POINTER(C.c_size_t)]),
+    "spb_heads_backward": (C.c_int, [C.POINTER(spb_heads_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "spb_encoder_heads": (C.c_int, [C.c_void_p, C.POINTER(spb_rotary), C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_float]),
+    "spb_muon_workspace_size": (C.c_int, [C.POINTER(spb_muon_tensor), C.c_int32, C.POINTER(C.c_size_t)]),
+    "spb_muon_step": (C.c_int, [C.POINTER(spb_muon_tensor), C.c_int32, C.POINTER(spb_muon_config), C.c_void_p, C.c_size_t, C.c_void_p]),
+    "spb_aggregate_muon_workspace_size": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_size_t)]),
+    "spb_aggregate_muon": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_void_p), C.POINTER(C.c_int32), C.POINTER(C.c_void_p),
+                                     C.POINTER(C.c_void_p), C.POINTER(spb_muon_config), C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
     "spb_set_kernel_timing": (C.c_int, [C.c_void_p, C.c_int32]),
     "spb_replay_kernel": (C.c_int, [C.c_void_p, C.c_char_p, C.c_int32, C.c_void_p]),
     "spb_read_kernel_timing": (C.c_int, [C.c_void_p, C.POINTER(spb_kernel_time), C.c_int32, C.POINTER(C.c_int32)]),
@@ -260,6 +295,150 @@ def spb_aggregate_update(m, depths, worker_grads, velocity, lr, momentum, weight
                                       int(bool(scale_lr)), C.c_void_p(stream)))
 
 
+def spb_rotary_sections(sections, base=10000.0, own_ladder=False, interleaved=False) -> spb_rotary:
+    """Rotary description: sections[a] pairs for axis a; see spb.h for the frequencies."""
+    out = spb_rotary()
+    _check(lib().spb_rotary_sections(C.byref(out), len(sections), (C.c_int32 * max(1, len(sections)))(*sections), base, int(bool(own_ladder)),
+                                     int(bool(interleaved))))
+    return out
+
+
+def _dtype_code(t) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return DTYPES["f32"]
+    if t.dtype == torch.bfloat16:
+        return DTYPES["bf16"]
+    raise ValueError(f"{t.dtype}: only float32 and bfloat16 are stored")
+
+
+def heads_desc(x, heads_q, y=None, dx=None, norm=False, eps=1e-5, rotary=None) -> spb_heads_desc:
+    """Description of a spb_heads_forward call on x and y, or a spb_heads_backward call on x, dy (passed as y) and dx: tensors
+    [batch, seq, heads, head_dim] of one dtype and any strides but that of the head's elements.  The first heads_q heads are queries, the
+    rest keys.  y and dx default to x's strides."""
+    d = spb_heads_desc()
+    batch, seq, heads, dim = x.shape
+    d.dtype, d.batch, d.seq, d.heads_q, d.heads_k, d.head_dim = _dtype_code(x), batch, seq, heads_q, heads - heads_q, dim
+    d.norm, d.eps = int(bool(norm)), eps
+    for name, t in (("x_stride", x), ("y_stride", x if y is None else y), ("dx_stride", x if dx is None else dx)):
+        if t.shape != x.shape or t.dtype != x.dtype:
+            raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, x is {tuple(x.shape)} of {x.dtype}")
+        if dim > 1 and t.stride(3) != 1:
+            raise ValueError(f"{name}: the elements of a head must be contiguous")
+        setattr(d, name, (C.c_int64 * 3)(*t.stride()[:3]))
+    if rotary is not None:
+        d.rotary = rotary
+    return d
+
+
+def _positions(desc, pos):
+    """(pointer, axis stride, batch stride) of positions [axes, batch, seq], int32; a batch dimension of 1 serves every sequence."""
+    if pos is None:
+        return None, 0, 0
+    import torch
+    if pos.dtype != torch.int32 or pos.dim() != 3:
+        raise ValueError(f"positions are int32 [axes, batch, seq], not {pos.dtype} {tuple(pos.shape)}")
+    axes, batch, seq = pos.shape
+    if axes < desc.rotary.axes or batch not in (1, desc.batch) or seq != desc.seq or (seq > 1 and pos.stride(2) != 1):
+        raise ValueError(f"positions {tuple(pos.shape)} (last stride {pos.stride(2)}) for {desc.rotary.axes} axes of {desc.batch} x {desc.seq} tokens")
+    return C.c_void_p(pos.data_ptr()), pos.stride(0), 0 if batch == 1 else pos.stride(1)
+
+
+def _weights(desc, t, name, dtype):
+    """Pointer of a [rows of weights, head_dim] tensor, dense."""
+    if t is None:
+        return None
+    shape = (2 if desc.heads_k else 1, desc.head_dim)
+    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, contiguous {shape} of {dtype} wanted")
+    return C.c_void_p(t.data_ptr())
+
+
+def spb_heads_forward(desc, x, y, pos, gamma, beta, stream):
+    where, axis_stride, batch_stride = _positions(desc, pos)
+    _check(lib().spb_heads_forward(C.byref(desc), _ptr(x), _ptr(y), where, axis_stride, batch_stride, _weights(desc, gamma, "gamma", x.dtype),
+                                   _weights(desc, beta, "beta", x.dtype), C.c_void_p(stream)))
+
+
+def spb_heads_workspace_size(desc) -> int:
+    n = C.c_size_t()
+    _check(lib().spb_heads_workspace_size(C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def spb_heads_backward(desc, x, dy, dx, pos, gamma, dgamma, dbeta, workspace, workspace_bytes, stream):
+    import torch
+    where, axis_stride, batch_stride = _positions(desc, pos)
+    _check(lib().spb_heads_backward(C.byref(desc), _ptr(x), _ptr(dy), _ptr(dx), where, axis_stride, batch_stride, _weights(desc, gamma, "gamma", dy.dtype),
+                                    _weights(desc, dgamma, "dgamma", torch.float32), _weights(desc, dbeta, "dbeta", torch.float32), _ptr(workspace),
+                                    workspace_bytes, C.c_void_p(stream)))
+
+
+def spb_encoder_heads(m, rotary, pos, norm=False, eps=1e-5):
+    """pos: [axes, batch or 1, seq] int32 on the device, for the model's batch and seq, which must outlive its passes; see spb.h."""
+    where, axis_stride, batch_stride = None, 0, 0
+    if pos is not None:
+        d = spb_heads_desc()
+        d.batch, d.seq = pos.shape[1], pos.shape[2]
+        if rotary is not None:
+            d.rotary = rotary
+        where, axis_stride, batch_stride = _positions(d, pos)
+    _check(lib().spb_encoder_heads(m, C.byref(rotary) if rotary is not None else None, where, axis_stride, batch_stride, int(bool(norm)), eps))
+
+
+def muon_config(lr, rms=0.2, momentum=0.95, nesterov=True, ns_steps=5, ns_eps=1e-7, beta1=0.9, beta2=0.95, adam_eps=1e-8, weight_decay=0.0,
+                step=1) -> spb_muon_config:
+    return spb_muon_config(lr, rms, momentum, ns_eps, beta1, beta2, adam_eps, weight_decay, step, int(bool(nesterov)), ns_steps)
+
+
+def _muon_tensors(tensors):
+    """ctypes list of tensors given as dict(w, m, v=None, grads=[...], blocks=0, rate_scale=1.0), and what keeps its arrays alive.  A
+    stack [blocks, rows, cols] is its matrices' rows one after the other; any other tensor has its first dimension as rows."""
+    import torch
+    arr = (spb_muon_tensor * max(1, len(tensors)))()
+    keep = []
+    for a, t in zip(arr, tensors):
+        w, m, v, grads, blocks = t["w"], t["m"], t.get("v"), t["grads"], t.get("blocks", 0)
+        for x in (w, m, v, *grads):
+            if x is not None and (x.shape != w.shape or not x.is_contiguous() or (x is not w and x.dtype != torch.float32)):
+                raise ValueError("m, v and gradients are contiguous float32 tensors of the parameter's shape, which is contiguous too")
+        stack = blocks >= 1 and w.dim() == 3 and w.shape[0] == blocks
+        rows = w.shape[0] * w.shape[1] if stack else (w.shape[0] if w.dim() else 1)
+        pointers = _ptr_array(grads)
+        keep.append(pointers)
+        a.w, a.m, a.v = w.data_ptr(), m.data_ptr(), None if v is None else v.data_ptr()
+        a.grads = C.cast(pointers, C.POINTER(C.c_void_p))
+        a.rows, a.cols = rows, w.numel() // rows if rows else 0
+        a.rate_scale, a.count, a.dtype, a.blocks = t.get("rate_scale", 1.0), len(grads), _dtype_code(w), blocks
+    return arr, keep
+
+
+def spb_muon_workspace_size(tensors) -> int:
+    arr, _keep = _muon_tensors(tensors)
+    n = C.c_size_t()
+    _check(lib().spb_muon_workspace_size(arr, len(tensors), C.byref(n)))
+    return n.value
+
+
+def spb_muon_step(tensors, config: spb_muon_config, workspace, workspace_bytes, stream):
+    arr, _keep = _muon_tensors(tensors)
+    _check(lib().spb_muon_step(arr, len(tensors), C.byref(config), _ptr(workspace), workspace_bytes, C.c_void_p(stream)))
+
+
+def spb_aggregate_muon_workspace_size(m, blocks) -> int:
+    n = C.c_size_t()
+    _check(lib().spb_aggregate_muon_workspace_size(m, (C.c_int32 * len(blocks))(*blocks), C.byref(n)))
+    return n.value
+
+
+def spb_aggregate_muon(m, depths, worker_grads, blocks, first, second, config: spb_muon_config, scale_lr, workspace, workspace_bytes, stream):
+    """worker_grads as in spb_aggregate_update; blocks, first, second: one entry per parameter (second: None for matrices)."""
+    n = len(depths)
+    flat = [g for per_worker in worker_grads for g in per_worker]
+    _check(lib().spb_aggregate_muon(m, n, (C.c_int32 * n)(*depths), _ptr_array(flat), (C.c_int32 * len(blocks))(*blocks), _ptr_array(first),
+                                    _ptr_array(second), C.byref(config), int(bool(scale_lr)), _ptr(workspace), workspace_bytes, C.c_void_p(stream)))
+
+
 def spb_set_kernel_timing(m, enable: bool):
     _check(lib().spb_set_kernel_timing(m, int(enable)))
 
@@ -304,7 +483,9 @@ def spb_schedule_tasks(jobs, n_machines: int, gamma: float = 0.0, capacity: floa
 class SpbModel:
     """Convenience holder: a model handle plus the torch tensors bound to it (memory and stream plumbing only)."""
 
-    def __init__(self, cfg: dict, params: dict, device="cuda:0"):
+    def __init__(self, cfg: dict, params: dict, device="cuda:0", positions=None):
+        """An encoder's cfg may hold rotary=dict(sections, base, own_ladder, interleaved) and qk_norm=eps (see spb_encoder_heads); positions:
+        int32 [axes, batch or 1, seq] of its tokens."""
         import torch
         self.torch = torch
         self.cfg = cfg
@@ -312,6 +493,12 @@ class SpbModel:
         if self.device.type != "cuda" or not torch.cuda.is_available():
             raise RuntimeError("the SPB path needs a GPU; there is no host fallback")
         self.handle = spb_model_create(desc_from_config(cfg))
+        if cfg.get("rotary") or cfg.get("qk_norm"):
+            rotary = spb_rotary_sections(**cfg["rotary"]) if cfg.get("rotary") else None
+            if positions is not None and (positions.shape[1] not in (1, cfg["batch"]) or positions.shape[2] != cfg["seq"]):
+                raise ValueError(f"positions {tuple(positions.shape)} for {cfg['batch']} x {cfg['seq']} tokens")
+            self.positions = None if positions is None else positions.to(self.device, torch.int32).contiguous()
+            spb_encoder_heads(self.handle, rotary, self.positions, norm=bool(cfg.get("qk_norm")), eps=cfg.get("qk_norm") or 1e-5)
         self.n_units = spb_num_units(self.handle)
         self.infos = [spb_param_info(self.handle, i) for i in range(spb_param_count(self.handle))]
         self.params, self.grads = [], []

@@ -203,9 +203,6 @@ int KernelTimer::read(spb_kernel_time* out, int cap, int* n_out) {
 
 using spb::set_error;
 
-#define SPB_REQUIRE(cond, code, ...) \
-  do { if (!(cond)) { set_error(__VA_ARGS__); return (code); } } while (0)
-
 static int depth_ok(const spb_model* m, int k, const char* who) {
   if (k < 0 || k > m->impl->num_units) { set_error("%s: depth %d outside 0..%d", who, k, m->impl->num_units); return SPB_ERR_DEPTH_RANGE; }
   return SPB_OK;

@@ -1,7 +1,7 @@
 // Transformer-encoder family: units = embedding | pre-LayerNorm layers | masked-token head.
 // Forward pass, stash plan and truncated backward pass (Sec. 1-2 of the paper).
 //
-//   layer:  u = LN1(x);  qkv = u Wqkv^T + b;  P = softmax(Q K^T / sqrt d);  ctx = P V;  h = x + ctx Wo^T + bo
+//   layer:  u = LN1(x);  qkv = u Wqkv^T + b;  [Q, K normed and turned by positions: spb_encoder_heads];  P = softmax(Q K^T / sqrt d);  ctx = P V;  h = x + ctx Wo^T + bo
 //           v = LN2(h);  z1 = v W1^T + b1;  f = gelu(z1);  out = h + f W2^T + b2
 //   head:   y = LN(x[loss rows]);  logits = y Wv^T + bv;  mean softmax cross-entropy
 //
@@ -18,7 +18,7 @@
 namespace spb {
 namespace {
 
-struct LayerBuf { size_t u, stats1, qkv, prob, ctx, h, stats2, v, z1, f; };
+struct LayerBuf { size_t u, stats1, qkv, qk, prob, ctx, h, stats2, v, z1, f; };
 
 class EncoderModel : public Model {
  public:
@@ -28,6 +28,12 @@ class EncoderModel : public Model {
     B = d.batch; S = d.seq; NL = d.layers; H = d.hidden; NH = d.heads; D = H / NH; F = d.ffn; V = d.vocab; R = d.loss_rows;
     M = B * S; Z = B * NH;
     num_units = NL + 2;
+    list_params();
+  }
+
+  void list_params() {
+    params.clear();
+    param_bytes_ = 0;
     auto add = [&](const std::string& name, int unit, std::vector<int64_t> shape) {
       ParamInfo p; p.name = name; p.unit = unit; p.dtype = dtype; p.shape = std::move(shape); params.push_back(p);
     };
@@ -37,6 +43,7 @@ class EncoderModel : public Model {
       const std::string pre = "layer" + std::to_string(i) + ".";
       add(pre + "ln1.weight", i + 1, {H}); add(pre + "ln1.bias", i + 1, {H});
       add(pre + "attn.qkv.weight", i + 1, {3 * H, H}); add(pre + "attn.qkv.bias", i + 1, {3 * H});
+      if (norm_) { add(pre + "attn.qknorm.weight", i + 1, {2, D}); add(pre + "attn.qknorm.bias", i + 1, {2, D}); }
       add(pre + "attn.out.weight", i + 1, {H, H}); add(pre + "attn.out.bias", i + 1, {H});
       add(pre + "ln2.weight", i + 1, {H}); add(pre + "ln2.bias", i + 1, {H});
       add(pre + "ffn.w1.weight", i + 1, {F, H}); add(pre + "ffn.w1.bias", i + 1, {F});
@@ -50,8 +57,10 @@ class EncoderModel : public Model {
   }
 
   enum { LN1W, LN1B, QKVW, QKVB, OUTW, OUTB, LN2W, LN2B, W1W, W1B, W2W, W2B };
-  int lp(int layer, int j) const { return 2 + 12 * layer + j; }
-  int hp(int j) const { return 2 + 12 * NL + j; }
+  int per_layer() const { return norm_ ? 14 : 12; }
+  int lp(int layer, int j) const { return 2 + per_layer() * layer + j + (norm_ && j >= OUTW ? 2 : 0); }
+  int np(int layer, int j) const { return 2 + per_layer() * layer + QKVB + 1 + j; }   // the norm of queries and keys: 0 weight, 1 bias
+  int hp(int j) const { return 2 + per_layer() * NL + j; }
   int ldz() const { return (int)align_up((size_t)V, 4); }
   int ldv() const { return (int)align_up((size_t)V, 8); }
 
@@ -73,6 +82,7 @@ class EncoderModel : public Model {
       LayerBuf b;
       b.u = take(mh); b.stats1 = take((size_t)M * 8); b.qkv = take(3 * mh); b.prob = take(zss * 2); b.ctx = take(mh);
       b.h = take(mh); b.stats2 = take((size_t)M * 8); b.v = take(mh); b.z1 = take(mf); b.f = take(mf);
+      b.qk = 0;
       return b;
     };
     const size_t ping[2] = {take(mh), take(mh)};
@@ -80,7 +90,10 @@ class EncoderModel : public Model {
     p.xout.assign(NL + 1, 0);
     p.layer.assign(NL, scratch);
     for (int u = 0; u <= NL; ++u) p.xout[u] = (u + 1 >= cut) ? take(mh) : ping[u & 1];  // kept if the unit above reads it in its backward pass
-    for (int i = 0; i < NL; ++i) if (i + 1 >= cut) p.layer[i] = take_layer();
+    for (int i = 0; i < NL; ++i) if (i + 1 >= cut) {
+      p.layer[i] = take_layer();
+      if (norm_) p.layer[i].qk = take(2 * mh);   // queries and keys before the norm, which its backward pass reads
+    }
     p.scores = scores_in_memory() ? take(zss * 4) : 0;
     p.y = take((size_t)R * H * 2); p.statsf = take((size_t)R * 8); p.logits = take((size_t)R * ldz() * 4);
     p.row_loss = take((size_t)R * 4); p.dlogits = take((size_t)R * ldv() * 2);
@@ -88,8 +101,10 @@ class EncoderModel : public Model {
     if (k >= 1) {
       p.dy = take((size_t)R * H * 2);
       // one per LayerNorm in the backward pass: their column sums are added up in one launch at the end
-      p.partial_bytes = align_up(std::max(layernorm_partial_floats(M, H), layernorm_partial_floats(R, H)) * 4, 256);
-      p.partial = take(p.partial_bytes * (size_t)(2 * std::min(k - 1, NL) + 1));
+      size_t floats = std::max(layernorm_partial_floats(M, H), layernorm_partial_floats(R, H));
+      if (norm_) floats = std::max(floats, heads_partial_floats(B, S, NH, D));
+      p.partial_bytes = align_up(floats * 4, 256);
+      p.partial = take(p.partial_bytes * (size_t)((norm_ ? 3 : 2) * std::min(k - 1, NL) + 1));
     }
     if (k >= 2) {
       // dF, dh and dqkv are read by weight gradients on the second stream: two of each, used by alternate layers
@@ -103,6 +118,28 @@ class EncoderModel : public Model {
   size_t workspace_size(int k) const override { return plan(k).total; }
   // Attention as products and softmax passes: only then do the float32 scores go to memory.
   bool scores_in_memory() const { return !attention_fused_accepts(S, D, 3 * H, H) && !attention_rows_accepts(S, D, 3 * H, H); }
+
+  int head_dim() const override { return D; }
+  void set_heads(const spb_rotary* rotary, const int32_t* pos, long long pos_axis_stride, long long pos_batch_stride, bool norm, float eps) override {
+    rotary_ = rotary ? *rotary : spb_rotary{};
+    pos_ = pos; pos_axis_stride_ = pos_axis_stride; pos_batch_stride_ = pos_batch_stride;
+    norm_ = norm; eps_ = eps;
+    list_params();
+    stashed_k = -1;
+  }
+  bool turns_heads() const { return norm_ || rotary_.pairs > 0; }
+  // The query and key blocks of rows of `row` elements, in place.
+  HeadsProblem heads(int layer, void* qk, int row) const {
+    HeadsProblem q;
+    q.dtype = dtype; q.batch = B; q.seq = S; q.heads_q = q.heads_k = NH; q.head_dim = D;
+    q.norm = norm_; q.eps = eps_;
+    q.pairs = rotary_.pairs; q.interleaved = rotary_.interleaved; q.axis = rotary_.axis; q.freq = rotary_.freq;
+    q.pos = pos_; q.pos_axis_stride = pos_axis_stride_; q.pos_batch_stride = pos_batch_stride_;
+    if (norm_) { q.gamma = param_ptrs[np(layer, 0)]; q.beta = param_ptrs[np(layer, 1)]; }
+    q.out = qk;
+    for (auto* s : {q.x_stride, q.dy_stride, q.out_stride}) { s[0] = (long long)S * row; s[1] = row; s[2] = D; }
+    return q;
+  }
 
   // ---- product helpers -------------------------------------------------------------------------
   GemmProblem linear(const void* a, int lda, int rows, const void* w, int n_out, int n_in, const void* bias, void* c, int ldc) const {
@@ -153,6 +190,12 @@ class EncoderModel : public Model {
       if (int rc = run("layernorm_fwd", 2 * mh, s, [&] {
             return launch_layernorm_fwd(xin, H, nullptr, M, H, P(LN1W), P(LN1B), w + b.u, H, reinterpret_cast<float*>(w + b.stats1), s); })) return rc;
       if (int rc = gemm(linear(w + b.u, H, M, P(QKVW), 3 * H, H, P(QKVB), w + b.qkv, 3 * H), s)) return rc;
+      if (turns_heads()) {
+        HeadsProblem q = heads(i, w + b.qkv, 3 * H);
+        q.x = w + b.qkv;
+        if (norm_ && i + 1 >= num_units - k) q.keep = w + b.qk;
+        if (int rc = run("heads_fwd", (q.keep ? 6 : 4) * mh, s, [&] { return launch_heads_forward(q, s); })) return rc;
+      }
       if (attention_fused_accepts(S, D, 3 * H, H)) {
         // one kernel per layer; P is written only where the backward pass will read it
         void* keep_prob = (i + 1 >= num_units - k) ? w + b.prob : nullptr;
@@ -227,7 +270,7 @@ class EncoderModel : public Model {
     // each leaves its partial sums in a buffer of its own and one launch at the end adds all of them up, instead of
     // two short kernels per layer on the chain.
     std::vector<ReduceTask> ln_sums;
-    ln_sums.reserve(2 * NL + 1);
+    ln_sums.reserve((norm_ ? 3 : 2) * NL + 1);
     auto next_partial = [&]() {
       ln_sums.emplace_back();
       return reinterpret_cast<float*>(w + p.partial + p.partial_bytes * (ln_sums.size() - 1));
@@ -352,6 +395,16 @@ class EncoderModel : public Model {
         if (int rc = gemm(dk, s)) return rc;
       }
       }
+      if (turns_heads()) {   // from the gradients of what attention saw to those of the projection
+        HeadsProblem q = heads(i, dqkv, 3 * H);
+        q.dy = dqkv;
+        if (norm_) {
+          q.x = w + b.qk;
+          q.x_stride[0] = (long long)S * 2 * H; q.x_stride[1] = 2 * H;
+          q.partial = next_partial(); q.dgamma = G(np(i, 0)); q.dbeta = G(np(i, 1));
+        }
+        if (int rc = run("heads_bwd", (norm_ ? 6 : 4) * mh, s, [&] { return launch_heads_backward(q, s, norm_ ? &ln_sums.back() : nullptr); })) return rc;
+      }
       {
         hipStream_t side = fork(s);   // and one for the attention half
         if (int rc = gemm(wgrad(dh, H, w + b.ctx, H, M, H, H, GP(OUTW), GP(OUTB)), side)) return rc;
@@ -407,6 +460,11 @@ class EncoderModel : public Model {
   const int32_t* ids_ = nullptr;
   const int32_t* rows_ = nullptr;
   size_t param_bytes_ = 0;
+  spb_rotary rotary_ = {};        // pairs = 0: none
+  const int32_t* pos_ = nullptr;
+  long long pos_axis_stride_ = 0, pos_batch_stride_ = 0;
+  bool norm_ = false;             // of query and key rows
+  float eps_ = 0.f;
   bool weights_in_hbm_ = false;   // by the time the step that is being enqueued reads them
 };
 

@@ -1,0 +1,594 @@
+// The rows of query and key heads between projection and attention: a layer norm of each head's row, a rotation of
+// its pairs by the token's positions, or both in one pass, and the gradient of that.
+//
+//   norm      xh = (x - mean) / sqrt(var + eps) over the head's elements;  n = gamma xh + beta
+//   rotation  pair j turns by t_j = freq_j * pos[axis_j]:  (u, v) -> (u cos t - v sin t, u sin t + v cos t)
+//   backward  g = the gradient turned by -t;  dbeta = sum g;  dgamma = sum g xh;  h = g gamma;
+//             dx = (h - mean(h) - xh mean(h xh)) / sqrt(var + eps)
+//
+// Memory-bound: every element is read once and written once, statistics are formed from the row in registers (the
+// backward pass forms them again rather than read them).  What threatens to bound it instead is the angles: cosine and
+// sine of a far position in enough bits take a few hundred instruction slots a pair.  So a workgroup takes all heads of a
+// few tokens and works the angles out once per token and pair, into LDS, where every head of the token reads them.
+//
+// An angle is formed as a fraction of a turn in float64: positions are whole numbers, so position times turns per unit, less
+// the nearest whole number, keeps 2^-53 * |position| turns (2^-22 at the far end of int32), and only the fraction in
+// [-1/2, 1/2] is rounded to float32.  Everything else is float32, rounded once where the result is stored.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "kernels.h"
+
+namespace spb {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+constexpr int kMaxTokensPerBlock = 16;
+
+struct bf16_t { uint16_t bits; };
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(bf16_t v) { return __uint_as_float(((uint32_t)v.bits) << 16); }
+__device__ __forceinline__ void store(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store(bf16_t* p, float v) { p->bits = bf16_round(v); }
+
+// elements of a 16-byte chunk
+template <typename T> struct Chunk;
+template <> struct Chunk<bf16_t> {
+  static constexpr int kN = 8;
+  static __device__ __forceinline__ void unpack(const u32x4& w, float (&f)[8]) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) { f[2 * d] = __uint_as_float(w[d] << 16); f[2 * d + 1] = __uint_as_float(w[d] & 0xFFFF0000u); }
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&f)[8]) {
+    u32x4 o;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) o[d] = bf16_pack2(f[2 * d], f[2 * d + 1]);
+    return o;
+  }
+};
+template <> struct Chunk<float> {
+  static constexpr int kN = 4;
+  static __device__ __forceinline__ void unpack(const u32x4& w, float (&f)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(w[e]);
+  }
+  static __device__ __forceinline__ u32x4 pack(const float (&f)[4]) {
+    u32x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(f[e]);
+    return o;
+  }
+};
+
+struct Args {
+  const void* x;          // forward: the input; backward: the forward pass's input (null without norm)
+  const void* dy;         // backward only
+  void* out;              // forward: y; backward: dx
+  void* keep;             // forward, optional: x once more, [token][heads][dim] dense
+  const int32_t* pos;
+  const void* gamma; const void* beta;
+  float* partial;         // backward with norm: [blocks][2][groups * dim]
+  long long pos_axis, pos_batch;
+  long long xs[3], gs[3], os[3];   // strides in elements (batch, token, head) of x, dy and out
+  int tokens, seq, heads_q, heads, dim, pairs, interleaved, norm, inverse, tokens_per_block;
+  float eps;
+  uint8_t axis[SPB_MAX_PAIRS];
+  double turns[SPB_MAX_PAIRS];     // turns per unit of position
+};
+
+struct Token { long long x, g, o; };
+
+// Offsets of the tokens of a block and the cosines and sines of their pairs, into LDS.
+__device__ __forceinline__ void load_tokens(const Args& a, unsigned first, int n, Token* tok, float2* cs) {
+  if ((int)threadIdx.x < n) {
+    const unsigned t = first + threadIdx.x, b = t / (unsigned)a.seq, s = t - b * a.seq;
+    tok[threadIdx.x] = Token{(long long)b * a.xs[0] + (long long)s * a.xs[1], (long long)b * a.gs[0] + (long long)s * a.gs[1], (long long)b * a.os[0] + (long long)s * a.os[1]};
+  }
+  for (int i = threadIdx.x; i < n * a.pairs; i += kThreads) {
+    const int k = i / a.pairs, j = i - k * a.pairs;
+    const unsigned t = first + k, b = t / (unsigned)a.seq, s = t - b * a.seq;
+    double turn = (double)a.pos[a.axis[j] * a.pos_axis + (long long)b * a.pos_batch + s] * a.turns[j];
+    turn -= rint(turn);
+    float sn, cn;
+    sincospif(2.f * (float)turn, &sn, &cn);
+    cs[i] = make_float2(cn, a.inverse ? -sn : sn);
+  }
+}
+
+// Which two chunks of its row lane l holds.  Pairs as halves: chunk l and the chunk its partners are in, as far as pairs reach, then the
+// rest two by two; interleaved pairs lie inside a chunk.
+__device__ __forceinline__ void chunks_of(int l, int rotated_half, int interleaved, int& c0, int& c1) {
+  if (interleaved) { c0 = 2 * l; c1 = 2 * l + 1; }
+  else if (l < rotated_half) { c0 = l; c1 = l + rotated_half; }
+  else { c0 = 2 * rotated_half + 2 * (l - rotated_half); c1 = c0 + 1; }
+}
+
+// Rotates the two chunks a lane holds; cs: the token's pairs.
+template <int V>
+__device__ __forceinline__ void turn(float (&u)[V], float (&v)[V], const float2* cs, int c0, int c1, int rotated, int interleaved) {
+  if (interleaved) {
+    if (c0 < rotated) {
+#pragma unroll
+      for (int e = 0; e < V; e += 2) {
+        const float2 t = cs[(c0 * V + e) >> 1];
+        const float p = u[e], q = u[e + 1];
+        u[e] = p * t.x - q * t.y; u[e + 1] = p * t.y + q * t.x;
+      }
+    }
+    if (c1 < rotated) {
+#pragma unroll
+      for (int e = 0; e < V; e += 2) {
+        const float2 t = cs[(c1 * V + e) >> 1];
+        const float p = v[e], q = v[e + 1];
+        v[e] = p * t.x - q * t.y; v[e + 1] = p * t.y + q * t.x;
+      }
+    }
+  } else if (c0 < rotated / 2) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float2 t = cs[c0 * V + e];
+      const float p = u[e], q = v[e];
+      u[e] = p * t.x - q * t.y; v[e] = p * t.y + q * t.x;
+    }
+  }
+}
+
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+template <int V>
+__device__ __forceinline__ float sum_of(const float (&u)[V], const float (&v)[V]) {
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < V; ++e) s += u[e] + v[e];
+  return s;
+}
+
+// mean and 1 / sqrt(var + eps) of a row spread over G lanes; u, v become x - mean (zero where the lane holds nothing).
+template <int G, int V>
+__device__ __forceinline__ float centre(float (&u)[V], float (&v)[V], bool has0, bool has1, float inv_dim, float eps) {
+  const float mean = group_sum<G>(sum_of(u, v)) * inv_dim;
+  float sq = 0.f;
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    u[e] = has0 ? u[e] - mean : 0.f;
+    v[e] = has1 ? v[e] - mean : 0.f;
+    sq += u[e] * u[e] + v[e] * v[e];
+  }
+  return 1.f / sqrtf(group_sum<G>(sq) * inv_dim + eps);
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void load_chunk(const T* p, bool has, float (&f)[V]) {
+  u32x4 w = {0u, 0u, 0u, 0u};
+  if (has) w = *reinterpret_cast<const u32x4*>(p);
+  Chunk<T>::unpack(w, f);
+}
+
+// Rows of whole 16-byte chunks: G lanes a row, two chunks a lane.  Also the backward pass without norm (a rotation by -t).
+template <typename T, int G>
+__global__ __launch_bounds__(kThreads) void heads_forward_kernel(Args a) {
+  constexpr int V = Chunk<T>::kN;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  Token* tok = reinterpret_cast<Token*>(lds);
+  float2* cs = reinterpret_cast<float2*>(lds + sizeof(Token) * kMaxTokensPerBlock);
+  const unsigned first = blockIdx.x * (unsigned)a.tokens_per_block;
+  const int n = min(a.tokens_per_block, a.tokens - (int)first);
+  load_tokens(a, first, n, tok, cs);
+  __syncthreads();
+  const int l = threadIdx.x % G, chunks = a.dim / V;
+  const int rotated = 2 * a.pairs / V, half = a.pairs ? rotated / 2 : chunks / 2;
+  int c0, c1;
+  chunks_of(l, half, a.interleaved, c0, c1);
+  const bool has0 = c0 < chunks, has1 = c1 < chunks;
+  const float inv_dim = 1.f / (float)a.dim;
+  for (int r = threadIdx.x / G; r < n * a.heads; r += kThreads / G) {
+    const int k = r / a.heads, h = r - k * a.heads;
+    const T* src = static_cast<const T*>(a.x) + tok[k].x + h * a.xs[2];
+    float u[V], v[V];
+    load_chunk(src + c0 * V, has0, u);
+    load_chunk(src + c1 * V, has1, v);
+    if (a.keep) {
+      T* dst = static_cast<T*>(a.keep) + ((size_t)(first + k) * a.heads + h) * a.dim;
+      if (has0) *reinterpret_cast<u32x4*>(dst + c0 * V) = Chunk<T>::pack(u);
+      if (has1) *reinterpret_cast<u32x4*>(dst + c1 * V) = Chunk<T>::pack(v);
+    }
+    if (a.norm) {
+      const float rstd = centre<G>(u, v, has0, has1, inv_dim, a.eps);
+      const int row = (h >= a.heads_q) * a.dim;
+      float g0[V], g1[V], b0[V], b1[V];
+      load_chunk(static_cast<const T*>(a.gamma) + row + c0 * V, has0, g0);
+      load_chunk(static_cast<const T*>(a.gamma) + row + c1 * V, has1, g1);
+      load_chunk(static_cast<const T*>(a.beta) + row + c0 * V, has0 && a.beta, b0);
+      load_chunk(static_cast<const T*>(a.beta) + row + c1 * V, has1 && a.beta, b1);
+#pragma unroll
+      for (int e = 0; e < V; ++e) { u[e] = g0[e] * (u[e] * rstd) + b0[e]; v[e] = g1[e] * (v[e] * rstd) + b1[e]; }
+    }
+    if (a.pairs) turn(u, v, cs + k * a.pairs, c0, c1, rotated, a.interleaved);
+    T* dst = static_cast<T*>(a.out) + tok[k].o + h * a.os[2];
+    if (has0) *reinterpret_cast<u32x4*>(dst + c0 * V) = Chunk<T>::pack(u);
+    if (has1) *reinterpret_cast<u32x4*>(dst + c1 * V) = Chunk<T>::pack(v);
+  }
+}
+
+// Backward pass with norm.  Workgroups walk over blocks of tokens and keep the sums for dgamma and dbeta of the elements their lanes hold
+// in registers, queries' and keys' apart; at the end each adds its lanes up through LDS in a fixed order and writes one partial row.
+template <typename T, int G>
+__global__ __launch_bounds__(kThreads) void heads_norm_backward_kernel(Args a) {
+  constexpr int V = Chunk<T>::kN;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  Token* tok = reinterpret_cast<Token*>(lds);
+  float2* cs = reinterpret_cast<float2*>(lds + sizeof(Token) * kMaxTokensPerBlock);
+  const int l = threadIdx.x % G, chunks = a.dim / V;
+  const int rotated = 2 * a.pairs / V, half = a.pairs ? rotated / 2 : chunks / 2;
+  int c0, c1;
+  chunks_of(l, half, a.interleaved, c0, c1);
+  const bool has0 = c0 < chunks, has1 = c1 < chunks;
+  const float inv_dim = 1.f / (float)a.dim;
+  float dgam[2][2][V], dbet[2][2][V];
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+#pragma unroll
+    for (int e = 0; e < V; ++e) dgam[g][0][e] = dgam[g][1][e] = dbet[g][0][e] = dbet[g][1][e] = 0.f;
+  for (unsigned first = blockIdx.x * (unsigned)a.tokens_per_block; first < (unsigned)a.tokens; first += gridDim.x * (unsigned)a.tokens_per_block) {
+    const int n = min(a.tokens_per_block, a.tokens - (int)first);
+    __syncthreads();
+    load_tokens(a, first, n, tok, cs);
+    __syncthreads();
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int heads = g ? a.heads - a.heads_q : a.heads_q, h0 = g ? a.heads_q : 0;
+      float g0[V], g1[V];
+      load_chunk(static_cast<const T*>(a.gamma) + g * a.dim + c0 * V, has0 && heads, g0);
+      load_chunk(static_cast<const T*>(a.gamma) + g * a.dim + c1 * V, has1 && heads, g1);
+      for (int r = threadIdx.x / G; r < n * heads; r += kThreads / G) {
+        const int k = r / heads, h = h0 + r - k * heads;
+        const T* src = static_cast<const T*>(a.x) + tok[k].x + h * a.xs[2];
+        const T* grad = static_cast<const T*>(a.dy) + tok[k].g + h * a.gs[2];
+        float u[V], v[V], p[V], q[V];
+        load_chunk(src + c0 * V, has0, u);
+        load_chunk(src + c1 * V, has1, v);
+        load_chunk(grad + c0 * V, has0, p);
+        load_chunk(grad + c1 * V, has1, q);
+        const float rstd = centre<G>(u, v, has0, has1, inv_dim, a.eps);
+        if (a.pairs) turn(p, q, cs + k * a.pairs, c0, c1, rotated, a.interleaved);
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          u[e] *= rstd; v[e] *= rstd;
+          dgam[g][0][e] += p[e] * u[e]; dgam[g][1][e] += q[e] * v[e];
+          dbet[g][0][e] += p[e]; dbet[g][1][e] += q[e];
+          p[e] *= g0[e]; q[e] *= g1[e];
+          s1 += p[e] + q[e];
+          s2 += p[e] * u[e] + q[e] * v[e];
+        }
+        const float m1 = group_sum<G>(s1) * inv_dim, m2 = group_sum<G>(s2) * inv_dim;
+#pragma unroll
+        for (int e = 0; e < V; ++e) { u[e] = (p[e] - m1 - u[e] * m2) * rstd; v[e] = (q[e] - m1 - v[e] * m2) * rstd; }
+        T* dst = static_cast<T*>(a.out) + tok[k].o + h * a.os[2];
+        if (has0) *reinterpret_cast<u32x4*>(dst + c0 * V) = Chunk<T>::pack(u);
+        if (has1) *reinterpret_cast<u32x4*>(dst + c1 * V) = Chunk<T>::pack(v);
+      }
+    }
+  }
+  // [lane groups][2][dim] floats of one group of heads at a time, added up in lane-group order
+  float* sums = reinterpret_cast<float*>(lds);
+  const int width = (a.heads > a.heads_q ? 2 : 1) * a.dim, slot = threadIdx.x / G;
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    if (g && a.heads == a.heads_q) break;   // uniform
+    __syncthreads();
+    float* mine = sums + slot * 2 * a.dim;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      if (has0) { mine[c0 * V + e] = dgam[g][0][e]; mine[a.dim + c0 * V + e] = dbet[g][0][e]; }
+      if (has1) { mine[c1 * V + e] = dgam[g][1][e]; mine[a.dim + c1 * V + e] = dbet[g][1][e]; }
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * a.dim; c += kThreads) {
+      float s = 0.f;
+      for (int i = 0; i < kThreads / G; ++i) s += sums[i * 2 * a.dim + c];
+      const int which = c >= a.dim;
+      a.partial[((size_t)blockIdx.x * 2 + which) * width + g * a.dim + c - which * a.dim] = s;
+    }
+  }
+}
+
+// Any head size, stride and alignment: a wavefront takes a row; lane l holds pairs l and l + 64 and elements l, l + 64, ... behind
+// the last pair.  The same arithmetic with loads and stores of single elements.
+struct Row {
+  float u[2], v[2], w[4];
+};
+struct Places {
+  int pu[2], pv[2], pw[4];   // element of the head, or -1
+  __device__ __forceinline__ void init(int lane, int dim, int pairs, int interleaved) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int j = lane + 64 * i;
+      pu[i] = j < pairs ? (interleaved ? 2 * j : j) : -1;
+      pv[i] = j < pairs ? (interleaved ? 2 * j + 1 : j + pairs) : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = 2 * pairs + lane + 64 * i;
+      pw[i] = e < dim ? e : -1;
+    }
+  }
+};
+template <typename T>
+__device__ __forceinline__ void load_row(const T* p, const Places& at, Row& r) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) { r.u[i] = at.pu[i] >= 0 ? to_float(p[at.pu[i]]) : 0.f; r.v[i] = at.pv[i] >= 0 ? to_float(p[at.pv[i]]) : 0.f; }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.w[i] = at.pw[i] >= 0 ? to_float(p[at.pw[i]]) : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ void store_row(T* p, const Places& at, const Row& r) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (at.pu[i] >= 0) { store(p + at.pu[i], r.u[i]); store(p + at.pv[i], r.v[i]); }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (at.pw[i] >= 0) store(p + at.pw[i], r.w[i]);
+}
+// f(element of r, element of s, whether the lane holds it)
+template <class F>
+__device__ __forceinline__ void each(const Places& at, Row& r, const Row& s, F&& f) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) { f(r.u[i], s.u[i], at.pu[i] >= 0); f(r.v[i], s.v[i], at.pv[i] >= 0); }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f(r.w[i], s.w[i], at.pw[i] >= 0);
+}
+__device__ __forceinline__ float centre_row(const Places& at, Row& r, float inv_dim, float eps) {
+  float s = 0.f;
+  each(at, r, r, [&](float& a, float, bool) { s += a; });
+  const float mean = group_sum<64>(s) * inv_dim;
+  float sq = 0.f;
+  each(at, r, r, [&](float& a, float, bool has) { a = has ? a - mean : 0.f; sq += a * a; });
+  return 1.f / sqrtf(group_sum<64>(sq) * inv_dim + eps);
+}
+__device__ __forceinline__ void turn_row(Row& r, const Places& at, const float2* cs, int lane) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (at.pu[i] < 0) continue;
+    const float2 t = cs[lane + 64 * i];
+    const float p = r.u[i], q = r.v[i];
+    r.u[i] = p * t.x - q * t.y; r.v[i] = p * t.y + q * t.x;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void heads_forward_any_kernel(Args a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  Token* tok = reinterpret_cast<Token*>(lds);
+  float2* cs = reinterpret_cast<float2*>(lds + sizeof(Token) * kMaxTokensPerBlock);
+  const unsigned first = blockIdx.x * (unsigned)a.tokens_per_block;
+  const int n = min(a.tokens_per_block, a.tokens - (int)first);
+  load_tokens(a, first, n, tok, cs);
+  __syncthreads();
+  const int lane = threadIdx.x & 63;
+  Places at;
+  at.init(lane, a.dim, a.pairs, a.interleaved);
+  const float inv_dim = 1.f / (float)a.dim;
+  for (int r = threadIdx.x >> 6; r < n * a.heads; r += kThreads / 64) {
+    const int k = r / a.heads, h = r - k * a.heads;
+    Row x;
+    load_row(static_cast<const T*>(a.x) + tok[k].x + h * a.xs[2], at, x);
+    if (a.keep) store_row(static_cast<T*>(a.keep) + ((size_t)(first + k) * a.heads + h) * a.dim, at, x);
+    if (a.norm) {
+      const float rstd = centre_row(at, x, inv_dim, a.eps);
+      const int row = (h >= a.heads_q) * a.dim;
+      Row w;
+      load_row(static_cast<const T*>(a.gamma) + row, at, w);
+      each(at, x, w, [&](float& v, float g, bool) { v = g * (v * rstd); });
+      if (a.beta) {
+        load_row(static_cast<const T*>(a.beta) + row, at, w);
+        each(at, x, w, [&](float& v, float b, bool) { v += b; });
+      }
+    }
+    if (a.pairs) turn_row(x, at, cs + k * a.pairs, lane);
+    store_row(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], at, x);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void heads_norm_backward_any_kernel(Args a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  Token* tok = reinterpret_cast<Token*>(lds);
+  float2* cs = reinterpret_cast<float2*>(lds + sizeof(Token) * kMaxTokensPerBlock);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Places at;
+  at.init(lane, a.dim, a.pairs, a.interleaved);
+  const float inv_dim = 1.f / (float)a.dim;
+  Row dgam[2], dbet[2];
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    each(at, dgam[g], dgam[g], [](float& v, float, bool) { v = 0.f; });
+    each(at, dbet[g], dbet[g], [](float& v, float, bool) { v = 0.f; });
+  }
+  for (unsigned first = blockIdx.x * (unsigned)a.tokens_per_block; first < (unsigned)a.tokens; first += gridDim.x * (unsigned)a.tokens_per_block) {
+    const int n = min(a.tokens_per_block, a.tokens - (int)first);
+    __syncthreads();
+    load_tokens(a, first, n, tok, cs);
+    __syncthreads();
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int heads = g ? a.heads - a.heads_q : a.heads_q, h0 = g ? a.heads_q : 0;
+      if (heads == 0) continue;   // uniform
+      Row gam;
+      load_row(static_cast<const T*>(a.gamma) + g * a.dim, at, gam);
+      for (int r = wave; r < n * heads; r += kThreads / 64) {
+        const int k = r / heads, h = h0 + r - k * heads;
+        Row x, d;
+        load_row(static_cast<const T*>(a.x) + tok[k].x + h * a.xs[2], at, x);
+        load_row(static_cast<const T*>(a.dy) + tok[k].g + h * a.gs[2], at, d);
+        const float rstd = centre_row(at, x, inv_dim, a.eps);
+        if (a.pairs) turn_row(d, at, cs + k * a.pairs, lane);
+        each(at, x, x, [&](float& v, float, bool) { v *= rstd; });
+        each(at, dbet[g], d, [](float& s, float v, bool) { s += v; });
+        Row dh = d;
+        each(at, dh, x, [](float& v, float xh, bool) { v *= xh; });
+        each(at, dgam[g], dh, [](float& s, float v, bool) { s += v; });
+        each(at, d, gam, [](float& v, float w, bool) { v *= w; });
+        float s1 = 0.f, s2 = 0.f;
+        each(at, d, x, [&](float& v, float xh, bool) { s1 += v; s2 += v * xh; });
+        const float m1 = group_sum<64>(s1) * inv_dim, m2 = group_sum<64>(s2) * inv_dim;
+        each(at, d, x, [&](float& v, float xh, bool) { v = (v - m1 - xh * m2) * rstd; });
+        store_row(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], at, d);
+      }
+    }
+  }
+  float* sums = reinterpret_cast<float*>(lds);   // [4 wavefronts][2][dim]
+  const int width = (a.heads > a.heads_q ? 2 : 1) * a.dim;
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    if (g && a.heads == a.heads_q) break;   // uniform
+    __syncthreads();
+    store_row(sums + wave * 2 * a.dim, at, dgam[g]);
+    store_row(sums + wave * 2 * a.dim + a.dim, at, dbet[g]);
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * a.dim; c += kThreads) {
+      const int which = c >= a.dim;
+      a.partial[((size_t)blockIdx.x * 2 + which) * width + g * a.dim + c - which * a.dim] =
+          ((sums[c] + sums[2 * a.dim + c]) + sums[4 * a.dim + c]) + sums[6 * a.dim + c];
+    }
+  }
+}
+
+struct Route {
+  int lanes = 0;             // lanes a row of the kernels of whole chunks, 0: the general kernels
+  int tokens_per_block = 1;
+  long long blocks = 0;
+  size_t lds = 0;
+};
+
+// Blocks of tokens so that a launch has some 2048 of them, or as many as there are tokens; a backward pass that adds up weight gradients keeps
+// at most 1024 workgroups, which walk over the blocks.
+constexpr long long kBlocksWanted = 2048;
+constexpr long long kBackwardBlocks = 1024;
+
+Route route_of(const HeadsProblem& q, bool sums) {
+  Route r;
+  const long long tokens = (long long)q.batch * q.seq;
+  long long per = tokens / kBlocksWanted;
+  r.tokens_per_block = (int)std::min<long long>(std::max<long long>(per, 1), kMaxTokensPerBlock);
+  r.blocks = (tokens + r.tokens_per_block - 1) / r.tokens_per_block;
+  if (sums) r.blocks = std::min(r.blocks, kBackwardBlocks);
+  const int v = q.dtype == DType::BF16 ? 8 : 4;
+  auto whole = [&](const long long (&s)[3]) { return s[0] % v == 0 && s[1] % v == 0 && s[2] % v == 0; };
+  const bool strides = whole(q.x_stride) && whole(q.out_stride) && (!q.dy || whole(q.dy_stride));
+  const uintptr_t bits = (uintptr_t)q.x | (uintptr_t)q.dy | (uintptr_t)q.out | (uintptr_t)q.gamma | (uintptr_t)q.beta | (uintptr_t)q.keep;
+  const bool pairs = q.interleaved ? 2 * q.pairs % v == 0 : q.pairs % v == 0;
+  if (q.head_dim % v == 0 && strides && (bits & 15) == 0 && pairs) {
+    r.lanes = 1;
+    while (r.lanes * 2 * v < q.head_dim) r.lanes *= 2;
+  }
+  r.lds = sizeof(Token) * kMaxTokensPerBlock + sizeof(float2) * (size_t)r.tokens_per_block * q.pairs;
+  if (sums) r.lds = std::max(r.lds, (size_t)(r.lanes ? kThreads / r.lanes : 4) * 2 * q.head_dim * sizeof(float));
+  return r;
+}
+
+Args args_of(const HeadsProblem& q, const Route& r, bool inverse) {
+  Args a = {};
+  a.x = q.x; a.dy = q.dy; a.out = q.out; a.keep = q.keep; a.pos = q.pos; a.gamma = q.gamma; a.beta = q.beta; a.partial = q.partial;
+  a.pos_axis = q.pos_axis_stride; a.pos_batch = q.pos_batch_stride;
+  for (int i = 0; i < 3; ++i) { a.xs[i] = q.x_stride[i]; a.gs[i] = q.dy_stride[i]; a.os[i] = q.out_stride[i]; }
+  a.tokens = q.batch * q.seq;
+  a.seq = q.seq; a.heads_q = q.heads_q; a.heads = q.heads_q + q.heads_k; a.dim = q.head_dim;
+  a.pairs = q.pairs; a.interleaved = q.pairs ? q.interleaved : 0; a.norm = q.norm; a.inverse = inverse; a.tokens_per_block = r.tokens_per_block;
+  a.eps = q.eps;
+  for (int j = 0; j < q.pairs; ++j) { a.axis[j] = (uint8_t)q.axis[j]; a.turns[j] = q.freq[j] / (2.0 * M_PI); }
+  return a;
+}
+
+template <typename F>
+hipError_t launch(F* kernel, const Route& r, const Args& a, hipStream_t s) {
+  if (r.lds > 64 * 1024)
+    if (hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kernel), r.lds); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)r.blocks), dim3(kThreads), r.lds, s, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_forward(const Route& r, const Args& a, hipStream_t s) {
+  switch (r.lanes) {
+    case 0: return launch(heads_forward_any_kernel<T>, r, a, s);
+    case 1: return launch(heads_forward_kernel<T, 1>, r, a, s);
+    case 2: return launch(heads_forward_kernel<T, 2>, r, a, s);
+    case 4: return launch(heads_forward_kernel<T, 4>, r, a, s);
+    case 8: return launch(heads_forward_kernel<T, 8>, r, a, s);
+    case 16: return launch(heads_forward_kernel<T, 16>, r, a, s);
+    case 32:
+      if constexpr (std::is_same_v<T, float>) return launch(heads_forward_kernel<T, 32>, r, a, s);
+      break;
+  }
+  return hipErrorInvalidValue;
+}
+template <typename T>
+hipError_t launch_norm_backward(const Route& r, const Args& a, hipStream_t s) {
+  switch (r.lanes) {
+    case 0: return launch(heads_norm_backward_any_kernel<T>, r, a, s);
+    case 1: return launch(heads_norm_backward_kernel<T, 1>, r, a, s);
+    case 2: return launch(heads_norm_backward_kernel<T, 2>, r, a, s);
+    case 4: return launch(heads_norm_backward_kernel<T, 4>, r, a, s);
+    case 8: return launch(heads_norm_backward_kernel<T, 8>, r, a, s);
+    case 16: return launch(heads_norm_backward_kernel<T, 16>, r, a, s);
+    case 32:
+      if constexpr (std::is_same_v<T, float>) return launch(heads_norm_backward_kernel<T, 32>, r, a, s);
+      break;
+  }
+  return hipErrorInvalidValue;
+}
+
+bool valid(const HeadsProblem& q) {
+  return q.batch > 0 && q.seq > 0 && q.heads_q > 0 && q.heads_k >= 0 && q.head_dim > 0 && q.head_dim <= SPB_MAX_HEAD_DIM && q.pairs >= 0 &&
+         2 * q.pairs <= q.head_dim && (long long)q.batch * q.seq <= 0x7FFFFFFFll && q.out;
+}
+
+}  // namespace
+
+hipError_t launch_heads_forward(const HeadsProblem& q, hipStream_t s) {
+  if (!valid(q) || !q.x) return hipErrorInvalidValue;
+  const Route r = route_of(q, false);
+  const Args a = args_of(q, r, false);
+  return q.dtype == DType::BF16 ? launch_forward<bf16_t>(r, a, s) : launch_forward<float>(r, a, s);
+}
+
+size_t heads_partial_floats(int batch, int seq, int heads_k, int head_dim) {
+  const long long tokens = (long long)batch * seq;
+  return (size_t)std::min(std::max<long long>(tokens, 1), kBackwardBlocks) * 2 * (heads_k ? 2 : 1) * head_dim;
+}
+
+hipError_t launch_heads_backward(const HeadsProblem& q, hipStream_t s, ReduceTask* deferred) {
+  if (!valid(q) || !q.dy) return hipErrorInvalidValue;
+  if (!q.norm) {   // a rotation back
+    HeadsProblem b = q;
+    b.x = q.dy; b.dy = nullptr; b.keep = nullptr; b.gamma = b.beta = nullptr;
+    for (int i = 0; i < 3; ++i) b.x_stride[i] = q.dy_stride[i];
+    const Route r = route_of(b, false);
+    const Args a = args_of(b, r, true);
+    return q.dtype == DType::BF16 ? launch_forward<bf16_t>(r, a, s) : launch_forward<float>(r, a, s);
+  }
+  if (!q.x || !q.partial || !q.dgamma || !q.dbeta) return hipErrorInvalidValue;
+  const Route r = route_of(q, true);
+  const Args a = args_of(q, r, true);
+  const hipError_t e = q.dtype == DType::BF16 ? launch_norm_backward<bf16_t>(r, a, s) : launch_norm_backward<float>(r, a, s);
+  if (e != hipSuccess) return e;
+  ReduceTask task;
+  task.kind = ReduceTask::kPairs;
+  task.partial = q.partial; task.count = (int)r.blocks; task.width = (q.heads_k ? 2 : 1) * q.head_dim;
+  task.out = q.dgamma; task.out_b = q.dbeta;
+  task.blocks = reduce_pairs_blocks(task.width);
+  if (deferred) { *deferred = task; return hipSuccess; }
+  return launch_unit_reduce(&task, 1, s);
+}
+
+}  // namespace spb

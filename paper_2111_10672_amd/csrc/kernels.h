@@ -8,6 +8,7 @@
 #include <mutex>
 #include <utility>
 
+#include "../../include/spb.h"
 #include "bf16_round.h"
 
 namespace spb {
@@ -281,6 +282,47 @@ struct AggregateTensor {
 };
 hipError_t launch_aggregate_update(const AggregateTensor* tensors, int n_tensors, DType param_dtype, float momentum,
                                    float weight_decay, hipStream_t stream);
+
+// The rows of query and key heads, normed and turned (heads.hip).  Strides in elements: batch, token, head.
+struct HeadsProblem {
+  DType dtype = DType::BF16;
+  int batch = 0, seq = 0, heads_q = 0, heads_k = 0, head_dim = 0;
+  int norm = 0, pairs = 0, interleaved = 0;
+  float eps = 0.f;
+  const int32_t* axis = nullptr;   // host, [pairs]
+  const double* freq = nullptr;    // host, [pairs]
+  const void* x = nullptr;         // forward: input; backward: the forward pass's input (with norm)
+  const void* dy = nullptr;        // backward
+  void* out = nullptr;             // forward: y; backward: dx
+  void* keep = nullptr;            // forward, optional: receives x, [tokens][heads][head_dim] dense
+  long long x_stride[3] = {}, dy_stride[3] = {}, out_stride[3] = {};
+  const int32_t* pos = nullptr;
+  long long pos_axis_stride = 0, pos_batch_stride = 0;
+  const void* gamma = nullptr;
+  const void* beta = nullptr;
+  float* partial = nullptr;        // backward with norm: scratch of heads_partial_floats(...) floats
+  float* dgamma = nullptr;
+  float* dbeta = nullptr;
+};
+hipError_t launch_heads_forward(const HeadsProblem& q, hipStream_t s);
+size_t heads_partial_floats(int batch, int seq, int heads_k, int head_dim);
+// With `deferred` the sums for dgamma and dbeta are left to a later launch_unit_reduce, as in launch_layernorm_bwd.
+hipError_t launch_heads_backward(const HeadsProblem& q, hipStream_t s, ReduceTask* deferred = nullptr);
+
+// One optimiser step, matrices orthogonalised, the rest AdamW (muon.hip); fields as in spb.h.
+struct MuonTensor {
+  void* w = nullptr;
+  float* m = nullptr;
+  float* v = nullptr;
+  const float* g[kMaxAggWorkers] = {};
+  long long rows = 0, cols = 0;
+  double rate = 0.0;
+  int count = 0;
+  DType dtype = DType::BF16;
+  int blocks = 0;
+};
+size_t muon_workspace_size(const MuonTensor* tensors, int n);
+hipError_t launch_muon_step(const MuonTensor* tensors, int n, const spb_muon_config& c, void* workspace, hipStream_t stream);
 
 }  // namespace spb
 

@@ -92,6 +92,9 @@ class Model {
   // with respect to that unit's output lies once a backward pass of depth exactly L - unit has run (the unit being
   // the lowest visited one, nothing has overwritten it).  Host-only.
   virtual void unit_io(int k, int unit, spb_buffer_view* input, spb_buffer_view* output_grad) const = 0;
+  // Encoders: elements of a head (0: the model has none), and what its query and key rows go through before attention (spb_encoder_heads).
+  virtual int head_dim() const { return 0; }
+  virtual void set_heads(const spb_rotary*, const int32_t*, long long, long long, bool, float) {}
 
   int num_units = 0;
   DType dtype = DType::BF16;
@@ -154,6 +157,10 @@ inline spb_buffer_view no_view() { spb_buffer_view v; v.offset = SPB_VIEW_NONE; 
 
 
 }  // namespace spb
+
+// Argument checks of the C entries (with spb::set_error in scope).
+#define SPB_REQUIRE(cond, code, ...) \
+  do { if (!(cond)) { set_error(__VA_ARGS__); return (code); } } while (0)
 
 struct spb_model {
   std::unique_ptr<spb::Model> impl;

@@ -110,6 +110,15 @@ CONFIGS = {
     "rows_attention_chain2_bf16": dict(family="encoder", dtype="bf16", batch=16, seq=264, layers=1, hidden=512, heads=8, ffn=64, vocab=97, loss_rows=60),
     # longer than those rows: batched products and softmax passes
     "long_attention_520_bf16": dict(family="encoder", dtype="bf16", batch=1, seq=520, layers=1, hidden=64, heads=1, ffn=64, vocab=97, loss_rows=60),
+    # query and key rows normed and turned by positions on three axes, in each of the three attention paths; one with the norm alone, one with the
+    # rotation alone (of part of each head, interleaved)
+    "qk_encoder_bf16": dict(family="encoder", dtype="bf16", batch=2, seq=40, layers=2, hidden=128, heads=2, ffn=136, vocab=97, loss_rows=23, qk_norm=1e-5,
+                            rotary=dict(sections=[8, 12, 12], base=10000.0, own_ladder=False, interleaved=False)),
+    "qk_long_encoder_bf16": dict(family="encoder", dtype="bf16", batch=2, seq=136, layers=1, hidden=128, heads=2, ffn=64, vocab=53, loss_rows=41, qk_norm=1e-6,
+                                 rotary=dict(sections=[16, 16], base=100.0, own_ladder=True, interleaved=False)),
+    "qk_norm_encoder_bf16": dict(family="encoder", dtype="bf16", batch=3, seq=24, layers=1, hidden=96, heads=4, ffn=64, vocab=53, loss_rows=11, qk_norm=1e-5),
+    "rotary_encoder_bf16": dict(family="encoder", dtype="bf16", batch=3, seq=24, layers=2, hidden=64, heads=4, ffn=64, vocab=53, loss_rows=11,
+                                rotary=dict(sections=[3, 1], base=10000.0, own_ladder=False, interleaved=True)),
     # a vocabulary large enough for the head's input gradient to be cut into k-slices and for the long-row loss kernel
     "big_vocab_encoder_bf16": dict(family="encoder", dtype="bf16", batch=2, seq=16, layers=1, hidden=64, heads=1,
                                    ffn=72, vocab=2311, loss_rows=9, depths=[0, 1, 2, 3]),

@@ -82,6 +82,8 @@ def tensor_specs(cfg: dict) -> list:
             specs += [
                 (pre + "ln1.weight", (h,), u, ("const", 1.0)), (pre + "ln1.bias", (h,), u, ("const", 0.0)),
                 (pre + "attn.qkv.weight", (3 * h, h), u, ("normal", std)), (pre + "attn.qkv.bias", (3 * h,), u, ("const", 0.0)),
+                *([(pre + "attn.qknorm.weight", (2, h // cfg["heads"]), u, ("const", 1.0)),
+                   (pre + "attn.qknorm.bias", (2, h // cfg["heads"]), u, ("const", 0.0))] if cfg.get("qk_norm") else []),
                 (pre + "attn.out.weight", (h, h), u, ("normal", std)), (pre + "attn.out.bias", (h,), u, ("const", 0.0)),
                 (pre + "ln2.weight", (h,), u, ("const", 1.0)), (pre + "ln2.bias", (h,), u, ("const", 0.0)),
                 (pre + "ffn.w1.weight", (f, h), u, ("normal", std)), (pre + "ffn.w1.bias", (f,), u, ("const", 0.0)),
@@ -131,7 +133,15 @@ def make_batch(cfg: dict, seed: int = 0) -> dict:
         # the positions that carry a loss: the first `rows` of a seeded permutation of all b * seq positions
         perm = _stream(seed, "batch/loss_rows").permutation(b * seq)[:rows].astype(np.int32)
         labels = _stream(seed, "batch/labels").integers(0, v, size=(rows,), dtype=np.int32)
-        return {"x": torch.from_numpy(ids), "loss_rows": torch.from_numpy(perm), "labels": torch.from_numpy(labels)}
+        out = {"x": torch.from_numpy(ids), "loss_rows": torch.from_numpy(perm), "labels": torch.from_numpy(labels)}
+        if cfg.get("rotary"):
+            # the sequences' positions on each axis: windows into something long, a grid whose last axis runs fastest
+            axes = len(cfg["rotary"]["sections"])
+            side = max(1, round(seq ** (1 / axes)))
+            grid = np.stack([np.arange(seq) // side ** (axes - 1 - a) % (side if a else seq) for a in range(axes)])
+            start = _stream(seed, "batch/positions").integers(0, 1000, size=(axes, b, 1))
+            out["positions"] = torch.from_numpy((grid[:, None, :] + start).astype(np.int32))
+        return out
     raise NotImplementedError(fam)
 
 
