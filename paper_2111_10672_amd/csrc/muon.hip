@@ -28,12 +28,9 @@ namespace {
 
 using gemm_detail::f32x16;
 using gemm_detail::f32x4;
-using gemm_detail::lds_offset;
 using gemm_detail::u32x4;
 using gemm_detail::xcd_tile;
-using gemm_dma_detail::fragments_ready;
 using gemm_dma_detail::krow_rot;
-using gemm_dma_detail::read_fragment;
 using gemm_dma_detail::wait_loads_and_barrier;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -48,7 +45,7 @@ struct Matrix {
   void* w;                 // first element of the matrix in its parameter
   const float* u;          // [rows, cols] dense
   const double* partial;   // [parts] sums of u^2
-  int parts, rows, cols, bf16;
+  int parts, rows, cols, bf16, vector;   // vector: 8 entries of a row are whole 16-byte pieces
   float keep, step, eps;   // w = keep * w - step * X
 };
 
@@ -169,7 +166,7 @@ __global__ __launch_bounds__(kThreads) void update_kernel(Table tab) {
     t.partial[(long long)mat * t.parts + part] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     if (part == 0)
       t.out[mat] = Matrix{t.bf16 ? (void*)(static_cast<uint16_t*>(t.w) + base) : (void*)(static_cast<float*>(t.w) + base), t.u + base,
-                          t.partial + (long long)mat * t.parts, t.parts, t.rows, t.cols, t.bf16, t.keep, t.step, tab.ns_eps};
+                          t.partial + (long long)mat * t.parts, t.parts, t.rows, t.cols, t.bf16, t.vector && t.cols % 8 == 0, t.keep, t.step, tab.ns_eps};
   }
 }
 
@@ -216,12 +213,12 @@ __device__ __forceinline__ void split8(const float (&v)[8], _Float16* p, size_t 
   }
 }
 template <int PLANES>
-__device__ __forceinline__ void join8(const _Float16* p, size_t plane, float (&v)[8]) {
-  const f16x8 hi = *reinterpret_cast<const f16x8*>(p);
+__device__ __forceinline__ void join8(const u32x4 (&w)[PLANES], float (&v)[8]) {
+  const f16x8 hi = __builtin_bit_cast(f16x8, w[0]);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = (float)hi[e];
   if constexpr (PLANES == 2) {
-    const f16x8 lo = *reinterpret_cast<const f16x8*>(p + plane);
+    const f16x8 lo = __builtin_bit_cast(f16x8, w[1]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += (float)lo[e] * (1.f / kLoScale);
   }
@@ -243,10 +240,24 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(Groups groups) {
   const bool tall = d.rows > d.cols;
   // rows of u: those of X, or, the matrix being tall, its columns
   const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
-  for (int k = threadIdx.x; k < 64 * 64; k += kThreads) {
-    const int r = k >> 6, c = k & 63;
-    tile_s[r][c] = r0 + r < d.rows && c0 + c < d.cols ? d.u[(size_t)(r0 + r) * d.cols + c0 + c] : 0.f;
+  f32x4 in[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = k * 16 + (threadIdx.x >> 4), c = (threadIdx.x & 15) * 4;
+    const float* src = d.u + (size_t)(r0 + r) * d.cols + c0 + c;
+    in[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (r0 + r >= d.rows) continue;
+    if (c0 + c + 4 <= d.cols && (d.cols & 3) == 0) in[k] = *reinterpret_cast<const f32x4*>(src);
+    else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c0 + c + e < d.cols) in[k][e] = src[e];
+    }
   }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tile_s[k * 16 + (threadIdx.x >> 4)][(threadIdx.x & 15) * 4 + e] = in[k][e];
   __syncthreads();
   const float scale = (float)((double)g.sigma / (sqrt((sums[0] + sums[1]) + (sums[2] + sums[3])) + (double)d.eps));
   const size_t plane = (size_t)g.mp * g.np;
@@ -260,10 +271,49 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(Groups groups) {
   }
 }
 
-// One operand panel of a tile on its way to LDS: ROWS rows with k contiguous (RowK), or k-rows of ROWS columns (KRow).
-template <int ROWS, Layout L>
+// w = keep * w - step * X for 8 entries of one row of the parameter; v: sigma X.
+__device__ __forceinline__ void apply8(const Matrix& d, float inv_sigma, const float (&v)[8], int row, int col) {
+  if (row >= d.rows || col >= d.cols) return;
+  const float step = d.step * inv_sigma;
+  const size_t at = (size_t)row * d.cols + col;
+  const bool whole = col + 8 <= d.cols && d.vector;
+  if (d.bf16) {
+    uint16_t* w = static_cast<uint16_t*>(d.w) + at;
+    if (whole) {
+      const u32x4 old = *reinterpret_cast<const u32x4*>(w);
+      u32x4 out;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        out[e] = bf16_pack2(d.keep * __uint_as_float(old[e] << 16) - step * v[2 * e], d.keep * __uint_as_float(old[e] & 0xFFFF0000u) - step * v[2 * e + 1]);
+      *reinterpret_cast<u32x4*>(w) = out;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < d.cols) w[e] = bf16_round(d.keep * bf(w[e]) - step * v[e]);
+    }
+  } else {
+    float* w = static_cast<float*>(d.w) + at;
+    if (whole) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        f32x4 old = *reinterpret_cast<const f32x4*>(w + 4 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) old[e] = d.keep * old[e] - step * v[4 * h + e];
+        *reinterpret_cast<f32x4*>(w + 4 * h) = old;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < d.cols) w[e] = d.keep * w[e] - step * v[e];
+    }
+  }
+}
+
+// One operand panel of a tile on its way to LDS: ROWS rows with k contiguous (RowK), or k-rows of ROWS columns (KRow), fetched by NW wavefronts.
+template <int ROWS, Layout L, int NW>
 struct Panel {
-  static constexpr int kInstr = ROWS / 32;   // four wavefronts of 64 chunks of 16 bytes
+  static constexpr int kInstr = ROWS / (8 * NW);   // direct-to-LDS instructions of a wavefront: 64 chunks of 16 bytes each
+  static_assert(ROWS % (8 * NW) == 0 && kInstr >= 1, "panel rows must fill whole wave instructions");
   const char* base;
   size_t step;
   uint32_t voff[kInstr];
@@ -272,7 +322,7 @@ struct Panel {
     base = reinterpret_cast<const char*>(L == Layout::RowK ? p + (size_t)row0 * ld : p + row0);
 #pragma unroll
     for (int i = 0; i < kInstr; ++i) {
-      const int slot = (i * 4 + wave) * 64 + lane;
+      const int slot = (i * NW + wave) * 64 + lane;
       if constexpr (L == Layout::RowK) {
         const int row = slot >> 3, pc = slot & 7;
         voff[i] = (uint32_t)row * ld * 2u + (uint32_t)((((pc ^ row ^ ((row >> 3) & 3)) & 7) << 3) * 2);   // the inverse of lds_offset
@@ -283,29 +333,38 @@ struct Panel {
       }
     }
   }
-  __device__ __forceinline__ void load(const char* at, char* tile, int wave) const {
-#pragma unroll
-    for (int i = 0; i < kInstr; ++i) {
-      const uint32_t dst = (uint32_t)(uintptr_t)(gemm_dma_detail::lds_ptr_t)(tile + (i * 4 + wave) * 1024);
-      asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff[i]), "s"(at), "s"(dst) : "m0", "memory");
-    }
+  __device__ __forceinline__ void load(int i, const char* at, char* tile, int wave) const {
+    const uint32_t dst = (uint32_t)(uintptr_t)(gemm_dma_detail::lds_ptr_t)(tile + (i * NW + wave) * 1024);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff[i]), "s"(at), "s"(dst) : "m0", "memory");
   }
 };
 
 enum Mode { kGram = 0, kPoly = 1, kUpdate = 2, kFinal = 3 };
 
-template <int BT, int STAGES>
-constexpr size_t product_lds = std::max((size_t)STAGES * 2 * BT * 128, (size_t)BT * (BT + 4) * 4);
-
-// kGram: A = X X^T.  kPoly: B = b A + c A A.  kUpdate: X' = a X + B X.  kFinal: the same, applied to the parameter.
-// Tiles of BT x BT by four wavefronts of BT/2 x BT/2; k in steps of 64 through a ring of STAGES tiles filled by direct-to-LDS loads.  The
-// matrices are padded to whole tiles with zeros, so nothing in the loop has an edge.
-template <int MODE, int PLANES, int BT, int STAGES>
-__global__ __launch_bounds__(kThreads) void product_kernel(Groups groups) {
-  constexpr int T = BT / 64;                  // 32 x 32 fragments of a wavefront, each way
-  constexpr int kStageBytes = 2 * BT * 128;
-  constexpr int kLoads = 2 * (BT / 32);
+// kGram: A = X X^T.  kPoly: B = a I + b A + c A A.  kUpdate: X' = B X.  kFinal: the same, applied to the parameter.
+// (a I inside B, so that the update reads nothing but the product's operands: X behind the tile loop once more was 200 MB of 24 matrices of 1024 x 4096, and
+// its latency stood between the loop and the stores.)
+// The matrices are padded to whole tiles with zeros, so nothing in the loop has an edge.
+//
+// Tile loop: a ring of STAGES tiles of 64 k, filled by direct-to-LDS loads.  A block is the MFMAs of one k-group (16 of k) on the
+// fragments fetched during the block before; between them the wave issues the LDS reads of the next k-group and its share of a
+// later tile's loads.  One barrier a tile, in front of its last k-group: by then the wave holds all of the tile in registers, so the
+// buffer may be overwritten, and its own loads of the next tile have landed, so everybody may read that.
+template <int MODE, int PLANES, int BT, int STAGES, int WAVES_M, int WAVES_N>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(Groups groups) {
+  constexpr int NW = WAVES_M * WAVES_N;
+  constexpr int WM = BT / WAVES_M, WN = BT / WAVES_N, TM = WM / 32, TN = WN / 32;
+  static_assert(WM % 32 == 0 && WN % 32 == 0, "wave tile is a multiple of 32 x 32");
+  constexpr int kPanelBytes = BT * 128, kStageBytes = 2 * PLANES * kPanelBytes;
   constexpr Layout LQ = MODE == kGram || MODE == kPoly ? Layout::RowK : Layout::KRow;
+  constexpr int PARTS = STAGES >= 3 ? 4 : 2;           // a tile's loads: in every block, or in the two after the barrier
+  constexpr int kSets = PLANES == 2 ? 3 : 1;           // products of planes
+  constexpr int kMfma = kSets * TM * TN, kReads = PLANES * (TM + TN), kReadsPerSlot = (kReads + kMfma - 1) / kMfma;
+  using SourceP = Panel<BT, Layout::RowK, NW>;
+  using SourceQ = Panel<BT, LQ, NW>;
+  constexpr int kLoads = 2 * PLANES * SourceP::kInstr;
+  static_assert((STAGES - 2) * kLoads < 64, "vmcnt range");
+  static_assert((size_t)NW * 32 * (WN + 4) * 4 <= (size_t)STAGES * kStageBytes, "epilogue staging fits in the ring");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   int mat, tile;
   const Group& g = group_of(groups, xcd_tile(blockIdx.x, gridDim.x), mat, tile);
@@ -321,166 +380,205 @@ __global__ __launch_bounds__(kThreads) void product_kernel(Groups groups) {
     ti = tile - tj * tiles_m;
   }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave & 1, wn = wave >> 1;
+  const int wm = wave % WAVES_M, wn = wave / WAVES_M;
   const size_t plane_x = (size_t)g.mp * g.np, plane_a = (size_t)g.mp * g.mp;
   const _Float16* x = g.x[0] + mat * PLANES * plane_x;
   _Float16* a = g.a + mat * PLANES * plane_a;
   _Float16* b = g.b + mat * PLANES * plane_a;
-  const _Float16* p = MODE == kGram ? x : MODE == kPoly ? a : b;
-  const _Float16* q = MODE == kPoly ? a : x;
-  const int ldp = MODE == kGram ? g.np : g.mp, ldq = MODE == kPoly ? g.mp : g.np;
   const size_t plane_p = (MODE == kGram ? plane_x : plane_a) * 2, plane_q = (MODE == kPoly ? plane_a : plane_x) * 2;   // bytes
-  const int k_tiles = (MODE == kGram ? g.np : g.mp) / kTileK;
-  const int n_steps = (PLANES == 2 ? 3 : 1) * k_tiles;
+  const int n = (MODE == kGram ? g.np : g.mp) / kTileK;
 
-  Panel<BT, Layout::RowK> sp;
-  Panel<BT, LQ> sq;
-  sp.init(p, ldp, ti * BT, wave, lane);
-  sq.init(q, ldq, tj * BT, wave, lane);
-  // the next tile to be requested: its step and, with two planes, which planes of the operands it multiplies
-  int next = 0, next_k = 0, pass = 0;
-  auto issue = [&]() {
-    char* stage = lds + (next % STAGES) * kStageBytes;
-    const char* at_p = sp.base + next_k * sp.step;
-    const char* at_q = sq.base + next_k * sq.step;
-    if constexpr (PLANES == 2) {
-      if (pass == 0) at_q += plane_q;
-      if (pass == 1) at_p += plane_p;
-    }
-    sp.load(at_p, stage, wave);
-    sq.load(at_q, stage + BT * 128, wave);
-    ++next;
-    if (++next_k == k_tiles) { next_k = 0; ++pass; }
-  };
+  SourceP sp;
+  SourceQ sq;
+  sp.init(MODE == kGram ? x : MODE == kPoly ? a : b, MODE == kGram ? g.np : g.mp, ti * BT, wave, lane);
+  sq.init(MODE == kPoly ? a : x, MODE == kPoly ? g.mp : g.np, tj * BT, wave, lane);
+  auto stage_of = [&](int t) { return lds + (t % STAGES) * kStageBytes; };
+  auto issue_part = [&](int t, int part) {
+    if (t >= n) return;
+    char* stage = stage_of(t);
 #pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s)
-    if (s < n_steps) issue();
-  f32x16 acc[T][T];
+    for (int pl = 0; pl < PLANES; ++pl)
 #pragma unroll
-  for (int i = 0; i < T; ++i)
-#pragma unroll
-    for (int j = 0; j < T; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-
-  for (int t = 0; t < n_steps; ++t) {
-    if (t + STAGES - 2 < n_steps) wait_loads_and_barrier<(STAGES - 2) * kLoads>();
-    else wait_loads_and_barrier<0>();
-    if (t + STAGES - 1 < n_steps) issue();
-    if (PLANES == 2 && t == 2 * k_tiles) {   // the products with remainders are complete
-#pragma unroll
-      for (int i = 0; i < T; ++i)
-#pragma unroll
-        for (int j = 0; j < T; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[i][j][r] *= 1.f / kLoScale;
-    }
-    const char* ps = lds + (t % STAGES) * kStageBytes;
-    const char* qs = ps + BT * 128;
-    constexpr int kBatch = T == 1 ? 4 : 2;
-#pragma unroll
-    for (int kb = 0; kb < 4; kb += kBatch) {
-      u32x4 pf[kBatch * T], qf[kBatch * T];
-#pragma unroll
-      for (int h = 0; h < kBatch; ++h) {
-#pragma unroll
-        for (int i = 0; i < T; ++i) pf[h * T + i] = read_fragment<BT, Layout::RowK>(ps, (wm * T + i) * 32, kb + h, lane);
-#pragma unroll
-        for (int j = 0; j < T; ++j) qf[h * T + j] = read_fragment<BT, LQ>(qs, (wn * T + j) * 32, kb + h, lane);
+      for (int i = 0; i < SourceP::kInstr; ++i) {
+        if ((2 * (pl * SourceP::kInstr + i)) % PARTS == part) sp.load(i, sp.base + t * sp.step + pl * plane_p, stage + pl * kPanelBytes, wave);
+        if ((2 * (pl * SourceP::kInstr + i) + 1) % PARTS == part) sq.load(i, sq.base + t * sq.step + pl * plane_q, stage + (PLANES + pl) * kPanelBytes, wave);
       }
-      if constexpr (LQ == Layout::KRow) fragments_ready(pf, qf);
+  };
+  f32x16 acc[TM][TN], acc_lo[PLANES == 2 ? TM : 1][PLANES == 2 ? TN : 1];
 #pragma unroll
-      for (int h = 0; h < kBatch; ++h)
+  for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int i = 0; i < T; ++i)
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
-          for (int j = 0; j < T; ++j)   // operands exchanged: a lane then holds runs of four columns of one row
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, qf[h * T + j]), __builtin_bit_cast(f16x8, pf[h * T + i]),
-                                                               acc[i][j], 0, 0, 0);
+      for (int r = 0; r < 16; ++r) {
+        acc[i][j][r] = 0.f;
+        if constexpr (PLANES == 2) acc_lo[i][j][r] = 0.f;
+      }
+
+  auto pin = [] { __builtin_amdgcn_sched_barrier(0); };   // the instruction scheduler moves nothing across this point
+  auto lds_done = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+  u32x4 fp[2][PLANES * TM], fq[2][PLANES * TN];
+  auto keep = [&](int set) {
+#pragma unroll
+    for (int i = 0; i < PLANES * TM; ++i) asm volatile("" : "+v"(fp[set][i]));
+#pragma unroll
+    for (int j = 0; j < PLANES * TN; ++j) asm volatile("" : "+v"(fq[set][j]));
+  };
+  using ReaderP = gemm_dma_detail::FragmentReader<BT, Layout::RowK, TM>;
+  using ReaderQ = gemm_dma_detail::FragmentReader<BT, LQ, TN>;
+  ReaderP reader_p;
+  ReaderQ reader_q;
+  reader_p.init(wm * WM, lane);
+  reader_q.init(wn * WN, lane);
+  struct At { uint32_t p[PLANES][ReaderP::kN], q[PLANES][ReaderQ::kN]; };
+  At at, next;                                             // the tile being multiplied, the tile after it
+  auto locate = [&](int t, At& where) {
+    const uint32_t base = (uint32_t)(uintptr_t)(gemm_dma_detail::lds_ptr_t)stage_of(t);
+#pragma unroll
+    for (int pl = 0; pl < PLANES; ++pl) { reader_p.at(base + pl * kPanelBytes, where.p[pl]); reader_q.at(base + (PLANES + pl) * kPanelBytes, where.q[pl]); }
+  };
+  // read number R of k-group KG into set S
+  auto fetch = [&](auto set, auto kg, auto r, const At& where) {
+    constexpr int S = decltype(set)::value, KG = decltype(kg)::value, R = decltype(r)::value;
+    if constexpr (R < PLANES * TM) fp[S][R] = ReaderP::template read<R % TM, KG>(where.p[R / TM]);
+    else if constexpr (R < kReads) fq[S][R - PLANES * TM] = ReaderQ::template read<(R - PLANES * TM) % TN, KG>(where.q[(R - PLANES * TM) / TN]);
+  };
+
+  // kPoly: the entries of A that 32 rows of the wave's tile are combined with, requested one strip ahead, the first here
+  constexpr int LD = WN + 4, kUnits = WN / 16;         // units of 8 columns of a lane
+  u32x4 held[2][kUnits][PLANES];
+  auto load_strip = [&](int i, u32x4 (&to)[kUnits][PLANES]) {
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) {
+      const int unit = k * 64 + lane, r = unit / (WN / 8), c = (unit % (WN / 8)) * 8;
+#pragma unroll
+      for (int pl = 0; pl < PLANES; ++pl)
+        to[k][pl] = *reinterpret_cast<const u32x4*>(a + pl * plane_a + (size_t)(ti * BT + wm * WM + i * 32 + r) * g.mp + tj * BT + wn * WN + c);
     }
+  };
+  if constexpr (MODE == kPoly) load_strip(0, held[0]);
+#pragma unroll
+  for (int t = 0; t < STAGES - 1; ++t)
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) issue_part(t, part);
+  issue_part(STAGES - 1, 0);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  pin();
+  __builtin_amdgcn_s_barrier();
+  pin();
+  locate(0, next);
+  gemm_detail::static_for<kReads>([&](auto r) { fetch(std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{}, r, next); });
+
+  for (int t = 0; t < n; ++t) {
+    const bool more = t + 1 < n;
+    locate(t, at);
+    gemm_detail::static_for<4>([&](auto blk_c) {
+      constexpr int blk = decltype(blk_c)::value, cur = blk & 1, nxt = cur ^ 1;
+      constexpr bool last = blk == 3;
+      lds_done();
+      keep(cur);
+      if constexpr (last) {
+        if (STAGES >= 3 && t + STAGES - 1 < n) __builtin_amdgcn_s_waitcnt(gemm_dma_detail::waitcnt_imm((STAGES - 2) * kLoads, 15));
+        else __builtin_amdgcn_s_waitcnt(gemm_dma_detail::waitcnt_imm(0, 15));
+        pin();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        locate(t + 1, next);
+      }
+      pin();
+      const bool fetching = !last || more;
+      const int load_tile = last ? t + STAGES : t + STAGES - 1;
+      constexpr int load_part = last ? 0 : blk + 1;
+      gemm_detail::static_for<kMfma>([&](auto idx_c) {
+        constexpr int idx = decltype(idx_c)::value;
+        constexpr int set = idx / (TM * TN), i = (idx / TN) % TM, j = idx % TN;
+        // with two planes: remainder x value, value x remainder, value x value.  (Operands exchanged: a lane then holds runs of four columns of one row.)
+        constexpr int qi = (PLANES == 2 && set == 0 ? TN : 0) + j, pi = (PLANES == 2 && set == 1 ? TM : 0) + i;
+        auto& into = [&]() -> f32x16& {
+          if constexpr (PLANES == 2 && set < 2) return acc_lo[i][j];
+          else return acc[i][j];
+        }();
+        into = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, fq[cur][qi]), __builtin_bit_cast(f16x8, fp[cur][pi]), into, 0, 0, 0);
+        if (fetching)
+          gemm_detail::static_for<kReadsPerSlot>([&](auto k) {
+            constexpr int r = idx * kReadsPerSlot + decltype(k)::value;
+            fetch(std::integral_constant<int, nxt>{}, std::integral_constant<int, last ? 0 : blk + 1>{}, std::integral_constant<int, r>{}, last ? next : at);
+          });
+        if constexpr (idx == 0 && load_part < PARTS) issue_part(load_tile, load_part);
+        pin();
+      });
+    });
   }
   wait_loads_and_barrier<0>();   // every wave is done with the ring
+  if constexpr (PLANES == 2) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] += acc_lo[i][j][r] * (1.f / kLoScale);
+  }
 
-  // The tile in float32 through LDS, so that what it is combined with and what it becomes move in 16-byte pieces.
-  constexpr int LD = BT + 4;
-  float* tile_s = reinterpret_cast<float*>(lds);
+  // 32 rows of the wave's tile at a time through its own part of LDS, so that what they are combined with and what they become move in
+  // 16-byte pieces: first row by row, then, for a mirror image or a tall parameter, column by column from what the first left there.
+  float* strip = reinterpret_cast<float*>(lds) + wave * (32 * LD);
+  const float inv_sigma = 1.f / g.sigma;
+  const Matrix d = MODE == kFinal ? g.matrices[mat] : Matrix{};
+  const bool tall = d.rows > d.cols;
+  const bool turn = MODE == kFinal ? tall : ti != tj;
 #pragma unroll
-  for (int i = 0; i < T; ++i)
+  for (int i = 0; i < TM; ++i) {
+    const int row0 = ti * BT + wm * WM + i * 32, col0 = tj * BT + wn * WN;
+    if constexpr (MODE == kPoly)
+      if (i + 1 < TM) load_strip(i + 1, held[(i + 1) & 1]);
 #pragma unroll
-    for (int j = 0; j < T; ++j)
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; r += 4)
-        *reinterpret_cast<f32x4*>(tile_s + ((wm * T + i) * 32 + (lane & 31)) * LD + (wn * T + j) * 32 + 2 * r + 4 * (lane >> 5)) =
-            f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
-  __syncthreads();
-  const float inv_sigma = 1.f / g.sigma;
-  constexpr int kUnits = BT * BT / 8;
-  if constexpr (MODE == kGram || MODE == kPoly) {
-    _Float16* out = MODE == kGram ? a : b;
-    auto finish = [&](float (&v)[8], size_t at) {
-      if constexpr (MODE == kGram) {
+        *reinterpret_cast<f32x4*>(strip + (lane & 31) * LD + j * 32 + 2 * r + 4 * (lane >> 5)) = f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
+    gemm_dma_detail::lanes_together();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= kTau * inv_sigma * inv_sigma;
-      } else {
+    for (int k = 0; k < kUnits; ++k) {
+      const int unit = k * 64 + lane, r = unit / (WN / 8), c = (unit % (WN / 8)) * 8;
+      float* at_s = strip + r * LD + c;
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(at_s), hi = *reinterpret_cast<const f32x4*>(at_s + 4);
+      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (MODE == kGram) v[e] *= kTau * inv_sigma * inv_sigma;
+        else if constexpr (MODE == kPoly) v[e] *= kC / kTau;
+        else v[e] *= 1.f / kTau;
+      }
+      if constexpr (MODE == kPoly) {
         float s[8];
-        join8<PLANES>(a + at, plane_a, s);
+        join8<PLANES>(held[i & 1][k], s);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = kB * s[e] + (kC / kTau) * v[e];
+        for (int e = 0; e < 8; ++e) v[e] += kB * s[e] + (row0 + r == col0 + c + e ? kA * kTau : 0.f);
       }
-      split8<PLANES>(v, out + at, plane_a);
-    };
-    for (int k = threadIdx.x; k < kUnits; k += kThreads) {
-      const int i = k / (BT / 8), j = (k % (BT / 8)) * 8;
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = tile_s[i * LD + j + e];
-      finish(v, (size_t)(ti * BT + i) * g.mp + tj * BT + j);
-    }
-    if (ti != tj)
-      for (int k = threadIdx.x; k < kUnits; k += kThreads) {   // its mirror image: 16 columns of the tile by 4 pieces of 8 rows at a time
-        const int c = k & 15, quad = (k >> 4) & 3, rest = k >> 6;
-        const int i = (rest % (BT / 16)) * 16 + c, j = ((rest / (BT / 16)) * 4 + quad) * 8;
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = tile_s[(j + e) * LD + i];
-        finish(v, (size_t)(tj * BT + i) * g.mp + ti * BT + j);
-      }
-  } else {
-    _Float16* next_x = g.x[1] + mat * PLANES * plane_x;
-    const Matrix d = MODE == kFinal ? g.matrices[mat] : Matrix{};
-    const bool tall = d.rows > d.cols;
-    for (int k = threadIdx.x; k < kUnits; k += kThreads) {
-      const int i = k / (BT / 8), j = (k % (BT / 8)) * 8;
-      const size_t at = (size_t)(ti * BT + i) * g.np + tj * BT + j;
-      float v[8], s[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = tile_s[i * LD + j + e];
-      join8<PLANES>(x + at, plane_x, s);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = kA * s[e] + (1.f / kTau) * v[e];
-      if constexpr (MODE == kUpdate) split8<PLANES>(v, next_x + at, plane_x);
-      else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) tile_s[i * LD + j + e] = v[e];   // (each entry by the thread that read it)
+      if constexpr (MODE == kGram) split8<PLANES>(v, a + (size_t)(row0 + r) * g.mp + col0 + c, plane_a);
+      else if constexpr (MODE == kPoly) split8<PLANES>(v, b + (size_t)(row0 + r) * g.mp + col0 + c, plane_a);
+      else if constexpr (MODE == kUpdate) split8<PLANES>(v, g.x[1] + mat * PLANES * plane_x + (size_t)(row0 + r) * g.np + col0 + c, plane_x);
+      else if (!turn) apply8(d, inv_sigma, v, row0 + r, col0 + c);
+      if (MODE != kUpdate && turn) {
+        *reinterpret_cast<f32x4*>(at_s) = f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4*>(at_s + 4) = f32x4{v[4], v[5], v[6], v[7]};
       }
     }
-    if constexpr (MODE == kFinal) {
-      __syncthreads();
-      const float step = d.step * inv_sigma;
-      for (int k = threadIdx.x; k < BT * BT; k += kThreads) {
-        const int hi = k / BT, lo = k % BT;                 // row of the parameter's tile, column
-        const int i = tall ? lo : hi, j = tall ? hi : lo;
-        const int row = (tall ? tj : ti) * BT + hi, col = (tall ? ti : tj) * BT + lo;
-        if (row >= d.rows || col >= d.cols) continue;
-        const size_t at = (size_t)row * d.cols + col;
-        const float v = tile_s[i * LD + j];
-        if (d.bf16) {
-          uint16_t* w = static_cast<uint16_t*>(d.w) + at;
-          *w = bf16_round(d.keep * bf(*w) - step * v);
-        } else {
-          float* w = static_cast<float*>(d.w) + at;
-          *w = d.keep * *w - step * v;
+    gemm_dma_detail::lanes_together();
+    if constexpr (MODE != kUpdate) {
+      if (turn) {   // uniform
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+          const int c = k * 16 + (lane >> 2), r = (lane & 3) * 8;
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = strip[(r + e) * LD + c];
+          if constexpr (MODE == kGram) split8<PLANES>(v, a + (size_t)(col0 + c) * g.mp + row0 + r, plane_a);
+          else if constexpr (MODE == kPoly) split8<PLANES>(v, b + (size_t)(col0 + c) * g.mp + row0 + r, plane_a);
+          else apply8(d, inv_sigma, v, col0 + c, row0 + r);
         }
+        gemm_dma_detail::lanes_together();
       }
     }
   }
@@ -488,9 +586,48 @@ __global__ __launch_bounds__(kThreads) void product_kernel(Groups groups) {
 
 // ---- plan -----------------------------------------------------------------------------------------------------------
 
+// What a product of `count` matrices in tiles of `tile` takes, in us, from these kernels' times over 1 to 64 matrices of 64 x 64 to 4096 x 4096: rounds of
+// workgroups over the 256 CUs, each a start and an end (2 to 8 us) and so much for every 64 of k.  Tiles of 64 and of 256 have a CU to
+// themselves (rings of 96 and 128 KB); those of 128 share one with another once there are more than CUs (24 products of 1024 x 4096 x 1024: 272 us so, 345 us
+// alone on a ring of four), and have it to themselves before (136 tiles over k = 2048: 26 against 23).  One float32 product of 1024 x 1024 x 1024: tiles
+// of 64 13 us, of 128 24; 16 of them: 175 and 112.  48 of 768 x 768 x 768: tiles of 128 62 us, of 256 53; their symmetric halves 44 and 53.
+double product_cost(long long tiles, int tile, int planes, int k) {
+  const double steps = k / 64;
+  auto rounds = [&](int at_once) { return (double)((tiles + at_once - 1) / at_once); };
+  if (planes == 2) return tile == 64 ? rounds(256) * (2.0 + 0.56 * steps) : rounds(256) * (5.0 + 1.44 * steps);
+  if (tile == 64) return rounds(256) * (2.8 + 0.29 * steps);
+  if (tile == 128) return tiles <= 256 ? 5.0 + 0.6 * steps : rounds(512) * (6.0 + 1.0 * steps);
+  return rounds(256) * (8.0 + 1.64 * steps);
+}
+
+long long tiles_of(int mode, int mp, int np, int tile) {
+  const long long m = mp / tile, n = np / tile;
+  return mode == kGram || mode == kPoly ? m * (m + 1) / 2 : m * n;
+}
+
+constexpr int largest_tile(int planes) { return planes == 2 ? 128 : 256; }
+
+// The cheapest tile among those that divide the padded sides, for all groups of a launch together.
+template <class Sizes>
+int pick_tile(int mode, int planes, int pad, const Sizes& groups, int n, double* cost = nullptr) {
+  int best = 64;
+  double least = 0.0;
+  for (int tile = 64; tile <= std::min(pad, largest_tile(planes)); tile *= 2) {
+    long long tiles = 0;
+    int k = 0;
+    for (int i = 0; i < n; ++i) {
+      tiles += tiles_of(mode, groups[i].mp, groups[i].np, tile) * groups[i].count;
+      k = std::max(k, mode == kGram ? groups[i].np : groups[i].mp);
+    }
+    const double c = product_cost(tiles, tile, planes, k);
+    if (tile == 64 || c < least) { best = tile; least = c; }
+  }
+  if (cost) *cost = least;
+  return best;
+}
+
 struct Plan {
-  struct Mat { int tensor, first; };                  // of a matrix tensor: its first entry of the matrix table
-  struct G { int planes, tile, mp, np, count = 0, first = 0; size_t x[2], a, b; float sigma; };
+  struct G { int planes, shorter, longer, pad, mp, np, count = 0, first = 0; size_t x[2], a, b; float sigma; };   // matrices of one shape and type
   std::vector<G> groups;
   std::vector<int> group_of_tensor, first_of_tensor, parts;
   std::vector<size_t> u, partial;
@@ -505,6 +642,61 @@ long long parts_of(long long numel, long long* chunk) {
   return (numel + c - 1) / c;
 }
 
+void pad_to(Plan::G& g, int pad) {
+  g.pad = pad;
+  g.mp = (g.shorter + pad - 1) / pad * pad;
+  g.np = (g.longer + pad - 1) / pad * pad;
+}
+
+// A step of the groups of one type, those of one padding launched together; a launch costs some 4 us.
+double step_cost(const std::vector<Plan::G>& groups, int planes) {
+  double sum = 0.0;
+  for (int pad = 64; pad <= largest_tile(planes); pad *= 2) {
+    std::vector<Plan::G> some;
+    for (const auto& g : groups)
+      if (g.planes == planes && g.pad == pad) some.push_back(g);
+    if (some.empty()) continue;
+    for (int mode : {kGram, kPoly, kUpdate}) {
+      double cost;
+      pick_tile(mode, planes, pad, some, (int)some.size(), &cost);
+      sum += cost + 4.0;
+    }
+  }
+  return sum;
+}
+
+// Sides padded to multiples of 64, 128 or 256, which is what lets a product use tiles of that size: each group as is cheapest for it alone, or
+// all alike, whichever makes the step cheaper.
+void choose_padding(std::vector<Plan::G>& groups, int planes) {
+  std::vector<Plan::G> best;
+  double least = 0.0;
+  auto consider = [&](std::vector<Plan::G> now) {
+    const double cost = step_cost(now, planes);
+    if (best.empty() || cost < least) { best = std::move(now); least = cost; }
+  };
+  std::vector<Plan::G> own = groups;
+  for (auto& g : own) {
+    if (g.planes != planes) continue;
+    double cheapest = 0.0;
+    Plan::G pick = g;
+    for (int pad = 64; pad <= largest_tile(planes); pad *= 2) {
+      Plan::G q = g;
+      pad_to(q, pad);
+      const double cost = step_cost({q}, planes);
+      if (pad == 64 || cost < cheapest) { pick = q; cheapest = cost; }
+    }
+    g = pick;
+  }
+  consider(own);
+  for (int pad = 64; pad <= largest_tile(planes); pad *= 2) {
+    std::vector<Plan::G> alike = groups;
+    for (auto& g : alike)
+      if (g.planes == planes) pad_to(g, pad);
+    consider(alike);
+  }
+  groups = std::move(best);
+}
+
 Plan make_plan(const MuonTensor* t, int n) {
   Plan p;
   size_t off = 0;
@@ -514,15 +706,12 @@ Plan make_plan(const MuonTensor* t, int n) {
   for (int i = 0; i < n; ++i) {
     if (t[i].blocks == 0) continue;
     const long long r = t[i].rows / t[i].blocks, c = t[i].cols;
-    const int shorter = (int)std::min(r, c), longer = (int)std::max(r, c);
-    const int tile = shorter > 64 ? 128 : 64;
     Plan::G g;
     g.planes = t[i].dtype == DType::F32 ? 2 : 1;
-    g.tile = tile;
-    g.mp = (shorter + tile - 1) / tile * tile;
-    g.np = (longer + tile - 1) / tile * tile;
+    g.shorter = (int)std::min(r, c);
+    g.longer = (int)std::max(r, c);
     size_t k = 0;
-    while (k < p.groups.size() && !(p.groups[k].planes == g.planes && p.groups[k].mp == g.mp && p.groups[k].np == g.np)) ++k;
+    while (k < p.groups.size() && !(p.groups[k].planes == g.planes && p.groups[k].shorter == g.shorter && p.groups[k].longer == g.longer)) ++k;
     if (k == p.groups.size()) p.groups.push_back(g);
     p.group_of_tensor[i] = (int)k;
     p.first_of_tensor[i] = p.groups[k].count;
@@ -531,6 +720,7 @@ Plan make_plan(const MuonTensor* t, int n) {
   }
   int first = 0;
   for (auto& g : p.groups) { g.first = first; first += g.count; }
+  for (int planes = 1; planes <= 2; ++planes) choose_padding(p.groups, planes);
   p.matrices = take(sizeof(Matrix) * (size_t)p.n_matrices);
   for (int i = 0; i < n; ++i) {
     if (t[i].blocks == 0) continue;
@@ -551,38 +741,55 @@ Plan make_plan(const MuonTensor* t, int n) {
   return p;
 }
 
-template <int MODE, int PLANES, int BT, int STAGES>
-hipError_t launch_product(Groups t, int blocks, hipStream_t s) {
-  auto* kernel = product_kernel<MODE, PLANES, BT, STAGES>;
-  constexpr size_t lds = product_lds<BT, STAGES>;
+template <int MODE, int PLANES, int BT, int STAGES, int WAVES_M, int WAVES_N>
+hipError_t launch_product(const Groups& t, int blocks, hipStream_t s) {
+  auto* kernel = product_kernel<MODE, PLANES, BT, STAGES, WAVES_M, WAVES_N>;
+  constexpr size_t lds = (size_t)STAGES * 2 * PLANES * BT * 128;
   if (lds > 64 * 1024)
     if (hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), lds, s, t);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * WAVES_M * WAVES_N), lds, s, t);
   return hipGetLastError();
 }
 
-template <int PLANES, int BT, int STAGES>
-hipError_t orthogonalise(Groups t, int steps, hipStream_t s) {
-  auto blocks_for = [&](auto per_matrix) {
-    int blocks = 0;
-    for (int i = 0; i < t.n; ++i) {
-      t.g[i].first_block = blocks;
-      t.g[i].per_matrix = per_matrix(t.g[i]);
-      blocks += t.g[i].per_matrix * t.g[i].count;
-    }
-    return blocks;
-  };
-  auto lower = [](const Group& g) { const int n = g.mp / BT; return n * (n + 1) / 2; };
-  auto all = [](const Group& g) { return (g.mp / BT) * (g.np / BT); };
-  int blocks = blocks_for([](const Group& g) { return (g.mp / 64) * (g.np / 64); });
+// Lays the workgroups of a launch out over the groups; the number of them, or -1 if it is too large for one.
+template <class F>
+int lay_out(Groups& t, F&& per_matrix) {
+  long long blocks = 0;
+  for (int i = 0; i < t.n; ++i) {
+    const long long per = per_matrix(t.g[i]);
+    if (blocks + per * t.g[i].count > 0x7FFFFFFFll) return -1;
+    t.g[i].first_block = (int)blocks;
+    t.g[i].per_matrix = (int)per;
+    blocks += per * t.g[i].count;
+  }
+  return (int)blocks;
+}
+
+template <int MODE, int PLANES>
+hipError_t product(Groups& t, int pad, hipStream_t s) {
+  const int tile = pick_tile(MODE, PLANES, pad, t.g, t.n);
+  const int blocks = lay_out(t, [&](const Group& g) { return tiles_of(MODE, g.mp, g.np, tile); });
+  if (blocks < 0) return hipErrorInvalidValue;
+  if constexpr (PLANES == 1) {
+    if (tile == 256) return launch_product<MODE, 1, 256, 2, 2, 4>(t, blocks, s);
+    if (tile == 128) return blocks <= 256 ? launch_product<MODE, 1, 128, 4, 2, 2>(t, blocks, s) : launch_product<MODE, 1, 128, 2, 2, 2>(t, blocks, s);
+    return launch_product<MODE, 1, 64, 6, 2, 2>(t, blocks, s);
+  } else {
+    if (tile == 128) return launch_product<MODE, 2, 128, 2, 2, 2>(t, blocks, s);
+    return launch_product<MODE, 2, 64, 4, 2, 2>(t, blocks, s);
+  }
+}
+
+template <int PLANES>
+hipError_t orthogonalise(Groups t, int pad, int steps, hipStream_t s) {
+  int blocks = lay_out(t, [](const Group& g) { return (long long)(g.mp / 64) * (g.np / 64); });
+  if (blocks < 0) return hipErrorInvalidValue;
   hipLaunchKernelGGL(normalise_kernel<PLANES>, dim3((unsigned)blocks), dim3(kThreads), 0, s, t);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   for (int k = 0; k < steps; ++k) {
-    blocks = blocks_for(lower);
-    if (hipError_t e = launch_product<kGram, PLANES, BT, STAGES>(t, blocks, s); e != hipSuccess) return e;
-    if (hipError_t e = launch_product<kPoly, PLANES, BT, STAGES>(t, blocks, s); e != hipSuccess) return e;
-    blocks = blocks_for(all);
-    const hipError_t e = k + 1 < steps ? launch_product<kUpdate, PLANES, BT, STAGES>(t, blocks, s) : launch_product<kFinal, PLANES, BT, STAGES>(t, blocks, s);
+    if (hipError_t e = product<kGram, PLANES>(t, pad, s); e != hipSuccess) return e;
+    if (hipError_t e = product<kPoly, PLANES>(t, pad, s); e != hipSuccess) return e;
+    const hipError_t e = k + 1 < steps ? product<kUpdate, PLANES>(t, pad, s) : product<kFinal, PLANES>(t, pad, s);
     if (e != hipSuccess) return e;
     for (int i = 0; i < t.n; ++i) std::swap(t.g[i].x[0], t.g[i].x[1]);
   }
@@ -633,13 +840,13 @@ hipError_t launch_muon_step(const MuonTensor* tensors, int n, const spb_muon_con
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   for (int planes = 1; planes <= 2; ++planes)
-    for (int tile = 64; tile <= 128; tile += 64) {
+    for (int pad = 64; pad <= largest_tile(planes); pad *= 2) {
       size_t k = 0;
       while (k < p.groups.size()) {
         Groups t = {};
         for (; k < p.groups.size() && t.n < kMaxGroups; ++k) {
           const Plan::G& s = p.groups[k];
-          if (s.planes != planes || s.tile != tile) continue;
+          if (s.planes != planes || s.pad != pad) continue;
           Group& d = t.g[t.n++];
           d.x[0] = reinterpret_cast<_Float16*>(ws + s.x[0]); d.x[1] = reinterpret_cast<_Float16*>(ws + s.x[1]);
           d.a = reinterpret_cast<_Float16*>(ws + s.a); d.b = reinterpret_cast<_Float16*>(ws + s.b);
@@ -647,8 +854,7 @@ hipError_t launch_muon_step(const MuonTensor* tensors, int n, const spb_muon_con
           d.mp = s.mp; d.np = s.np; d.count = s.count; d.sigma = s.sigma;
         }
         if (t.n == 0) break;
-        const hipError_t e = tile == 128 ? (planes == 1 ? orthogonalise<1, 128, 2>(t, c.ns_steps, stream) : orthogonalise<2, 128, 2>(t, c.ns_steps, stream))
-                                         : (planes == 1 ? orthogonalise<1, 64, 3>(t, c.ns_steps, stream) : orthogonalise<2, 64, 3>(t, c.ns_steps, stream));
+        const hipError_t e = planes == 1 ? orthogonalise<1>(t, pad, c.ns_steps, stream) : orthogonalise<2>(t, pad, c.ns_steps, stream);
         if (e != hipSuccess) return e;
       }
     }
