@@ -1,6 +1,7 @@
 """ctypes binding of libspb.so.  Same names as the C ABI; no arithmetic happens here."""
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 import struct
@@ -303,13 +304,27 @@ def spb_rotary_sections(sections, base=10000.0, own_ladder=False, interleaved=Fa
     return out
 
 
+_STORED = None      # torch's type -> dtype code (torch is imported by whoever has a tensor)
+
+
+def _stored():
+    global _STORED
+    if _STORED is None:
+        import torch
+        _STORED = {torch.float32: DTYPES["f32"], torch.bfloat16: DTYPES["bf16"]}
+    return _STORED
+
+
 def _dtype_code(t) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return DTYPES["f32"]
-    if t.dtype == torch.bfloat16:
-        return DTYPES["bf16"]
-    raise ValueError(f"{t.dtype}: only float32 and bfloat16 are stored")
+    code = _stored().get(t.dtype)
+    if code is None:
+        raise ValueError(f"{t.dtype}: only float32 and bfloat16 are stored")
+    return code
+
+
+# Filled in C in one go: field by field through ctypes a description took 12 us, twice the small kernels behind it.
+_HEADS = struct.Struct("<7if9q")       # spb_heads_desc up to its rotary
+assert _HEADS.size == spb_heads_desc.rotary.offset
 
 
 def heads_desc(x, heads_q, y=None, dx=None, norm=False, eps=1e-5, rotary=None) -> spb_heads_desc:
@@ -317,73 +332,80 @@ def heads_desc(x, heads_q, y=None, dx=None, norm=False, eps=1e-5, rotary=None) -
     [batch, seq, heads, head_dim] of one dtype and any strides but that of the head's elements.  The first heads_q heads are queries, the
     rest keys.  y and dx default to x's strides."""
     d = spb_heads_desc()
-    batch, seq, heads, dim = x.shape
-    d.dtype, d.batch, d.seq, d.heads_q, d.heads_k, d.head_dim = _dtype_code(x), batch, seq, heads_q, heads - heads_q, dim
-    d.norm, d.eps = int(bool(norm)), eps
-    for name, t in (("x_stride", x), ("y_stride", x if y is None else y), ("dx_stride", x if dx is None else dx)):
-        if t.shape != x.shape or t.dtype != x.dtype:
-            raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, x is {tuple(x.shape)} of {x.dtype}")
-        if dim > 1 and t.stride(3) != 1:
-            raise ValueError(f"{name}: the elements of a head must be contiguous")
-        setattr(d, name, (C.c_int64 * 3)(*t.stride()[:3]))
+    shape, dtype, sx = x.shape, x.dtype, x.stride()
+    batch, seq, heads, dim = shape
+    strides = [sx, sx, sx]
+    for i, t in ((1, y), (2, dx)):
+        if t is not None:
+            if t.shape != shape or t.dtype != dtype:
+                raise ValueError(f"{'x y dx'.split()[i]}: {tuple(t.shape)} of {t.dtype}, x is {tuple(shape)} of {dtype}")
+            strides[i] = t.stride()
+    sy, sd = strides[1:]
+    if dim > 1 and not sx[3] == sy[3] == sd[3] == 1:
+        raise ValueError("the elements of a head must be contiguous")
+    _HEADS.pack_into(d, 0, _dtype_code(x), batch, seq, heads_q, heads - heads_q, dim, 1 if norm else 0, eps, *sx[:3], *sy[:3], *sd[:3])
     if rotary is not None:
         d.rotary = rotary
     return d
 
 
 def _positions(desc, pos):
-    """(pointer, axis stride, batch stride) of positions [axes, batch, seq], int32; a batch dimension of 1 serves every sequence."""
+    """(address, axis stride, batch stride) of positions [axes, batch, seq], int32; a batch dimension of 1 serves every sequence."""
     if pos is None:
         return None, 0, 0
     import torch
     if pos.dtype != torch.int32 or pos.dim() != 3:
         raise ValueError(f"positions are int32 [axes, batch, seq], not {pos.dtype} {tuple(pos.shape)}")
-    axes, batch, seq = pos.shape
-    if axes < desc.rotary.axes or batch not in (1, desc.batch) or seq != desc.seq or (seq > 1 and pos.stride(2) != 1):
-        raise ValueError(f"positions {tuple(pos.shape)} (last stride {pos.stride(2)}) for {desc.rotary.axes} axes of {desc.batch} x {desc.seq} tokens")
-    return C.c_void_p(pos.data_ptr()), pos.stride(0), 0 if batch == 1 else pos.stride(1)
+    (axes, batch, seq), (by_axis, by_batch, by_token) = pos.shape, pos.stride()
+    if axes < desc.rotary.axes or batch not in (1, desc.batch) or seq != desc.seq or (seq > 1 and by_token != 1):
+        raise ValueError(f"positions {tuple(pos.shape)} (last stride {by_token}) for {desc.rotary.axes} axes of {desc.batch} x {desc.seq} tokens")
+    return pos.data_ptr(), by_axis, 0 if batch == 1 else by_batch
 
 
 def _weights(desc, t, name, dtype):
-    """Pointer of a [rows of weights, head_dim] tensor, dense."""
+    """Address of a [rows of weights, head_dim] tensor, dense."""
     if t is None:
         return None
     shape = (2 if desc.heads_k else 1, desc.head_dim)
-    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, contiguous {shape} of {dtype} wanted")
-    return C.c_void_p(t.data_ptr())
+    return t.data_ptr()
+
+
+def _address(t):
+    return None if t is None else t if isinstance(t, int) else t.data_ptr()
 
 
 def spb_heads_forward(desc, x, y, pos, gamma, beta, stream):
-    where, axis_stride, batch_stride = _positions(desc, pos)
-    _check(lib().spb_heads_forward(C.byref(desc), _ptr(x), _ptr(y), where, axis_stride, batch_stride, _weights(desc, gamma, "gamma", x.dtype),
-                                   _weights(desc, beta, "beta", x.dtype), C.c_void_p(stream)))
+    where, by_axis, by_batch = _positions(desc, pos)
+    _check(lib().spb_heads_forward(desc, x.data_ptr(), y.data_ptr(), where, by_axis, by_batch, _weights(desc, gamma, "gamma", x.dtype),
+                                   _weights(desc, beta, "beta", x.dtype), stream))
 
 
 def spb_heads_workspace_size(desc) -> int:
     n = C.c_size_t()
-    _check(lib().spb_heads_workspace_size(C.byref(desc), C.byref(n)))
+    _check(lib().spb_heads_workspace_size(desc, C.byref(n)))
     return n.value
 
 
 def spb_heads_backward(desc, x, dy, dx, pos, gamma, dgamma, dbeta, workspace, workspace_bytes, stream):
     import torch
-    where, axis_stride, batch_stride = _positions(desc, pos)
-    _check(lib().spb_heads_backward(C.byref(desc), _ptr(x), _ptr(dy), _ptr(dx), where, axis_stride, batch_stride, _weights(desc, gamma, "gamma", dy.dtype),
-                                    _weights(desc, dgamma, "dgamma", torch.float32), _weights(desc, dbeta, "dbeta", torch.float32), _ptr(workspace),
-                                    workspace_bytes, C.c_void_p(stream)))
+    where, by_axis, by_batch = _positions(desc, pos)
+    _check(lib().spb_heads_backward(desc, _address(x), _address(dy), _address(dx), where, by_axis, by_batch, _weights(desc, gamma, "gamma", dy.dtype),
+                                    _weights(desc, dgamma, "dgamma", torch.float32), _weights(desc, dbeta, "dbeta", torch.float32), _address(workspace),
+                                    workspace_bytes, stream))
 
 
 def spb_encoder_heads(m, rotary, pos, norm=False, eps=1e-5):
     """pos: [axes, batch or 1, seq] int32 on the device, for the model's batch and seq, which must outlive its passes; see spb.h."""
-    where, axis_stride, batch_stride = None, 0, 0
+    where, by_axis, by_batch = None, 0, 0
     if pos is not None:
         d = spb_heads_desc()
         d.batch, d.seq = pos.shape[1], pos.shape[2]
         if rotary is not None:
             d.rotary = rotary
-        where, axis_stride, batch_stride = _positions(d, pos)
-    _check(lib().spb_encoder_heads(m, C.byref(rotary) if rotary is not None else None, where, axis_stride, batch_stride, int(bool(norm)), eps))
+        where, by_axis, by_batch = _positions(d, pos)
+    _check(lib().spb_encoder_heads(m, C.byref(rotary) if rotary is not None else None, where, by_axis, by_batch, int(bool(norm)), eps))
 
 
 def muon_config(lr, rms=0.2, momentum=0.95, nesterov=True, ns_steps=5, ns_eps=1e-7, beta1=0.9, beta2=0.95, adam_eps=1e-8, weight_decay=0.0,
@@ -391,26 +413,32 @@ def muon_config(lr, rms=0.2, momentum=0.95, nesterov=True, ns_steps=5, ns_eps=1e
     return spb_muon_config(lr, rms, momentum, ns_eps, beta1, beta2, adam_eps, weight_decay, step, int(bool(nesterov)), ns_steps)
 
 
+_MUON = struct.Struct("<4Q2qd4i")      # spb_muon_tensor
+assert _MUON.size == C.sizeof(spb_muon_tensor)
+
+
 def _muon_tensors(tensors):
     """ctypes list of tensors given as dict(w, m, v=None, grads=[...], blocks=0, rate_scale=1.0), and what keeps its arrays alive.  A
     stack [blocks, rows, cols] is its matrices' rows one after the other; any other tensor has its first dimension as rows."""
     import torch
+    f32 = torch.float32
     arr = (spb_muon_tensor * max(1, len(tensors)))()
-    keep = []
-    for a, t in zip(arr, tensors):
+    pointers = array.array("Q", [g.data_ptr() for t in tensors for g in t["grads"]])
+    at = pointers.buffer_info()[0]
+    for i, t in enumerate(tensors):
         w, m, v, grads, blocks = t["w"], t["m"], t.get("v"), t["grads"], t.get("blocks", 0)
-        for x in (w, m, v, *grads):
-            if x is not None and (x.shape != w.shape or not x.is_contiguous() or (x is not w and x.dtype != torch.float32)):
-                raise ValueError("m, v and gradients are contiguous float32 tensors of the parameter's shape, which is contiguous too")
-        stack = blocks >= 1 and w.dim() == 3 and w.shape[0] == blocks
-        rows = w.shape[0] * w.shape[1] if stack else (w.shape[0] if w.dim() else 1)
-        pointers = _ptr_array(grads)
-        keep.append(pointers)
-        a.w, a.m, a.v = w.data_ptr(), m.data_ptr(), None if v is None else v.data_ptr()
-        a.grads = C.cast(pointers, C.POINTER(C.c_void_p))
-        a.rows, a.cols = rows, w.numel() // rows if rows else 0
-        a.rate_scale, a.count, a.dtype, a.blocks = t.get("rate_scale", 1.0), len(grads), _dtype_code(w), blocks
-    return arr, keep
+        shape = w.shape
+        good = w.is_contiguous()
+        for x in (m, *grads) if v is None else (m, v, *grads):
+            good = good and x.dtype == f32 and x.shape == shape and x.is_contiguous()
+        if not good:
+            raise ValueError("m, v and gradients are contiguous float32 tensors of the parameter's shape, which is contiguous too")
+        stack = blocks >= 1 and len(shape) == 3 and shape[0] == blocks
+        rows = shape[0] * shape[1] if stack else (shape[0] if shape else 1)
+        _MUON.pack_into(arr, i * _MUON.size, w.data_ptr(), m.data_ptr(), 0 if v is None else v.data_ptr(), at, rows, w.numel() // rows if rows else 0,
+                        t.get("rate_scale", 1.0), len(grads), _dtype_code(w), blocks, 0)
+        at += 8 * len(grads)
+    return arr, pointers
 
 
 def spb_muon_workspace_size(tensors) -> int:
@@ -422,7 +450,7 @@ def spb_muon_workspace_size(tensors) -> int:
 
 def spb_muon_step(tensors, config: spb_muon_config, workspace, workspace_bytes, stream):
     arr, _keep = _muon_tensors(tensors)
-    _check(lib().spb_muon_step(arr, len(tensors), C.byref(config), _ptr(workspace), workspace_bytes, C.c_void_p(stream)))
+    _check(lib().spb_muon_step(arr, len(tensors), config, _address(workspace), workspace_bytes, stream))
 
 
 def spb_aggregate_muon_workspace_size(m, blocks) -> int:

@@ -7,7 +7,8 @@
 //             dx = (h - mean(h) - xh mean(h xh)) / sqrt(var + eps)
 //
 // Memory-bound: every element is read once and written once, statistics are formed from the row in registers (the
-// backward pass forms them again rather than read them).  What threatens to bound it instead is the angles: cosine and
+// backward pass forms them again rather than read them).  32792 tokens of 32 heads of 128 in bfloat16, normed and half of each head turned: 107 us, 5.0 TB/s;
+// backward, 16384 tokens of 24 + 8 heads of 128 normed and turned: 91 us and 4 us for the sums, 4.2 TB/s.  What threatens to bound it instead is the angles: cosine and
 // sine of a far position in enough bits take a few hundred instruction slots a pair.  So a workgroup takes all heads of a
 // few tokens and works the angles out once per token and pair, into LDS, where every head of the token reads them.
 //
@@ -74,7 +75,7 @@ struct Args {
   float* partial;         // backward with norm: [blocks][2][groups * dim]
   long long pos_axis, pos_batch;
   long long xs[3], gs[3], os[3];   // strides in elements (batch, token, head) of x, dy and out
-  int tokens, seq, heads_q, heads, dim, pairs, interleaved, norm, inverse, tokens_per_block;
+  int tokens, seq, heads_q, heads, dim, pairs, interleaved, norm, inverse, tokens_per_block, tokens_per_block_k;
   float eps;
   uint8_t axis[SPB_MAX_PAIRS];
   double turns[SPB_MAX_PAIRS];     // turns per unit of position
@@ -166,17 +167,34 @@ __device__ __forceinline__ float centre(float (&u)[V], float (&v)[V], bool has0,
   return 1.f / sqrtf(group_sum<G>(sq) * inv_dim + eps);
 }
 
-template <typename T, int V>
-__device__ __forceinline__ void load_chunk(const T* p, bool has, float (&f)[V]) {
-  u32x4 w = {0u, 0u, 0u, 0u};
-  if (has) w = *reinterpret_cast<const u32x4*>(p);
-  Chunk<T>::unpack(w, f);
+// Which token of a block and which of `heads` heads row r is: r < 2^20, so float32 divides it exactly.
+__device__ __forceinline__ void place_of(int r, int heads, float inv_heads, int& token, int& head) {
+  token = (int)(((float)r + 0.5f) * inv_heads);
+  head = r - token * heads;
 }
 
-// Rows of whole 16-byte chunks: G lanes a row, two chunks a lane.  Also the backward pass without norm (a rotation by -t).
+// The two 16-byte chunks of a row that a lane holds, as they lie in memory.
+struct Pair { u32x4 c[2]; };
+template <typename T>
+__device__ __forceinline__ Pair load_pair(const T* row, int c0, int c1, bool has0, bool has1) {
+  constexpr int V = Chunk<T>::kN;
+  Pair p = {};
+  if (has0) p.c[0] = *reinterpret_cast<const u32x4*>(row + c0 * V);
+  if (has1) p.c[1] = *reinterpret_cast<const u32x4*>(row + c1 * V);
+  return p;
+}
+template <typename T>
+__device__ __forceinline__ void store_pair(T* row, const Pair& p, int c0, int c1, bool has0, bool has1) {
+  constexpr int V = Chunk<T>::kN;
+  if (has0) *reinterpret_cast<u32x4*>(row + c0 * V) = p.c[0];
+  if (has1) *reinterpret_cast<u32x4*>(row + c1 * V) = p.c[1];
+}
+
+// Rows of whole 16-byte chunks: G lanes a row, two chunks a lane.  Also the backward pass without norm (a rotation by -t).  With norm, queries and
+// keys one after the other, so that a lane holds the weights of its elements; the next row is requested before this one is worked on.
 template <typename T, int G>
 __global__ __launch_bounds__(kThreads) void heads_forward_kernel(Args a) {
-  constexpr int V = Chunk<T>::kN;
+  constexpr int V = Chunk<T>::kN, S = kThreads / G;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   Token* tok = reinterpret_cast<Token*>(lds);
   float2* cs = reinterpret_cast<float2*>(lds + sizeof(Token) * kMaxTokensPerBlock);
@@ -190,40 +208,57 @@ __global__ __launch_bounds__(kThreads) void heads_forward_kernel(Args a) {
   chunks_of(l, half, a.interleaved, c0, c1);
   const bool has0 = c0 < chunks, has1 = c1 < chunks;
   const float inv_dim = 1.f / (float)a.dim;
-  for (int r = threadIdx.x / G; r < n * a.heads; r += kThreads / G) {
-    const int k = r / a.heads, h = r - k * a.heads;
-    const T* src = static_cast<const T*>(a.x) + tok[k].x + h * a.xs[2];
-    float u[V], v[V];
-    load_chunk(src + c0 * V, has0, u);
-    load_chunk(src + c1 * V, has1, v);
-    if (a.keep) {
-      T* dst = static_cast<T*>(a.keep) + ((size_t)(first + k) * a.heads + h) * a.dim;
-      if (has0) *reinterpret_cast<u32x4*>(dst + c0 * V) = Chunk<T>::pack(u);
-      if (has1) *reinterpret_cast<u32x4*>(dst + c1 * V) = Chunk<T>::pack(v);
-    }
+  for (int g = 0; g < (a.norm ? 2 : 1); ++g) {
+    const int heads = !a.norm ? a.heads : g ? a.heads - a.heads_q : a.heads_q, h0 = g ? a.heads_q : 0, rows = n * heads;
+    if (rows == 0) break;
+    const float inv_heads = 1.f / (float)heads;
+    auto request = [&](int r) {
+      int k, h;
+      place_of(min(r, rows - 1), heads, inv_heads, k, h);
+      return load_pair(static_cast<const T*>(a.x) + tok[k].x + (h0 + h) * a.xs[2], c0, c1, has0, has1);
+    };
+    Pair next = request(threadIdx.x / G), gam = {}, bet = {};
     if (a.norm) {
-      const float rstd = centre<G>(u, v, has0, has1, inv_dim, a.eps);
-      const int row = (h >= a.heads_q) * a.dim;
-      float g0[V], g1[V], b0[V], b1[V];
-      load_chunk(static_cast<const T*>(a.gamma) + row + c0 * V, has0, g0);
-      load_chunk(static_cast<const T*>(a.gamma) + row + c1 * V, has1, g1);
-      load_chunk(static_cast<const T*>(a.beta) + row + c0 * V, has0 && a.beta, b0);
-      load_chunk(static_cast<const T*>(a.beta) + row + c1 * V, has1 && a.beta, b1);
-#pragma unroll
-      for (int e = 0; e < V; ++e) { u[e] = g0[e] * (u[e] * rstd) + b0[e]; v[e] = g1[e] * (v[e] * rstd) + b1[e]; }
+      gam = load_pair(static_cast<const T*>(a.gamma) + g * a.dim, c0, c1, has0, has1);
+      if (a.beta) bet = load_pair(static_cast<const T*>(a.beta) + g * a.dim, c0, c1, has0, has1);
     }
-    if (a.pairs) turn(u, v, cs + k * a.pairs, c0, c1, rotated, a.interleaved);
-    T* dst = static_cast<T*>(a.out) + tok[k].o + h * a.os[2];
-    if (has0) *reinterpret_cast<u32x4*>(dst + c0 * V) = Chunk<T>::pack(u);
-    if (has1) *reinterpret_cast<u32x4*>(dst + c1 * V) = Chunk<T>::pack(v);
+    for (int r = threadIdx.x / G; r < rows; r += S) {
+      int k, h;
+      place_of(r, heads, inv_heads, k, h);
+      h += h0;
+      const Pair now = next;
+      next = request(r + S);
+      if (a.keep) store_pair(static_cast<T*>(a.keep) + ((size_t)(first + k) * a.heads + h) * a.dim, now, c0, c1, has0, has1);
+      float u[V], v[V];
+      Chunk<T>::unpack(now.c[0], u);
+      Chunk<T>::unpack(now.c[1], v);
+      if (a.norm) {
+        const float rstd = centre<G>(u, v, has0, has1, inv_dim, a.eps);
+        float w[V], z[V];
+        Chunk<T>::unpack(gam.c[0], w);
+        Chunk<T>::unpack(bet.c[0], z);
+#pragma unroll
+        for (int e = 0; e < V; ++e) u[e] = w[e] * (u[e] * rstd) + z[e];
+        Chunk<T>::unpack(gam.c[1], w);
+        Chunk<T>::unpack(bet.c[1], z);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = w[e] * (v[e] * rstd) + z[e];
+      }
+      if (a.pairs) turn(u, v, cs + k * a.pairs, c0, c1, rotated, a.interleaved);
+      Pair out;
+      out.c[0] = Chunk<T>::pack(u);
+      out.c[1] = Chunk<T>::pack(v);
+      store_pair(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], out, c0, c1, has0, has1);
+    }
   }
 }
 
-// Backward pass with norm.  Workgroups walk over blocks of tokens and keep the sums for dgamma and dbeta of the elements their lanes hold
-// in registers, queries' and keys' apart; at the end each adds its lanes up through LDS in a fixed order and writes one partial row.
+// Backward pass with norm, queries (blockIdx.y = 0) and keys apart.  Workgroups walk over blocks of tokens and keep the sums for dgamma and dbeta of the
+// elements their lanes hold in registers (one kernel for both kinds of head held twice the sums: two wavefronts a SIMD instead of four, 4096 tokens of
+// 12 + 12 heads of 64 16.4 us); at the end each adds its lanes up through LDS in a fixed order and writes its part of a partial row.
 template <typename T, int G>
 __global__ __launch_bounds__(kThreads) void heads_norm_backward_kernel(Args a) {
-  constexpr int V = Chunk<T>::kN;
+  constexpr int V = Chunk<T>::kN, S = kThreads / G;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   Token* tok = reinterpret_cast<Token*>(lds);
   float2* cs = reinterpret_cast<float2*>(lds + sizeof(Token) * kMaxTokensPerBlock);
@@ -233,71 +268,107 @@ __global__ __launch_bounds__(kThreads) void heads_norm_backward_kernel(Args a) {
   chunks_of(l, half, a.interleaved, c0, c1);
   const bool has0 = c0 < chunks, has1 = c1 < chunks;
   const float inv_dim = 1.f / (float)a.dim;
-  float dgam[2][2][V], dbet[2][2][V];
+  const int g = blockIdx.y, heads = g ? a.heads - a.heads_q : a.heads_q, h0 = g ? a.heads_q : 0, per_block = g ? a.tokens_per_block_k : a.tokens_per_block;
+  const float inv_heads = 1.f / (float)heads;
+  const Pair gam = load_pair(static_cast<const T*>(a.gamma) + g * a.dim, c0, c1, has0, has1);
+  float dgam[2][V], dbet[2][V];
 #pragma unroll
-  for (int g = 0; g < 2; ++g)
-#pragma unroll
-    for (int e = 0; e < V; ++e) dgam[g][0][e] = dgam[g][1][e] = dbet[g][0][e] = dbet[g][1][e] = 0.f;
-  for (unsigned first = blockIdx.x * (unsigned)a.tokens_per_block; first < (unsigned)a.tokens; first += gridDim.x * (unsigned)a.tokens_per_block) {
-    const int n = min(a.tokens_per_block, a.tokens - (int)first);
+  for (int e = 0; e < V; ++e) dgam[0][e] = dgam[1][e] = dbet[0][e] = dbet[1][e] = 0.f;
+  for (unsigned first = blockIdx.x * (unsigned)per_block; first < (unsigned)a.tokens; first += gridDim.x * (unsigned)per_block) {
+    const int n = min(per_block, a.tokens - (int)first), rows = n * heads;
     __syncthreads();
     load_tokens(a, first, n, tok, cs);
     __syncthreads();
+    struct Both { Pair x, dy; };
+    auto request = [&](int r) {
+      int k, h;
+      place_of(min(r, rows - 1), heads, inv_heads, k, h);
+      return Both{load_pair(static_cast<const T*>(a.x) + tok[k].x + (h0 + h) * a.xs[2], c0, c1, has0, has1),
+                  load_pair(static_cast<const T*>(a.dy) + tok[k].g + (h0 + h) * a.gs[2], c0, c1, has0, has1)};
+    };
+    Both next = request(threadIdx.x / G);
+    for (int r = threadIdx.x / G; r < rows; r += S) {
+      int k, h;
+      place_of(r, heads, inv_heads, k, h);
+      h += h0;
+      const Both now = next;
+      next = request(r + S);
+      float u[V], v[V], p[V], q[V], w[V];
+      Chunk<T>::unpack(now.x.c[0], u);
+      Chunk<T>::unpack(now.x.c[1], v);
+      Chunk<T>::unpack(now.dy.c[0], p);
+      Chunk<T>::unpack(now.dy.c[1], q);
+      const float rstd = centre<G>(u, v, has0, has1, inv_dim, a.eps);
+      if (a.pairs) turn(p, q, cs + k * a.pairs, c0, c1, rotated, a.interleaved);
+      float s1 = 0.f, s2 = 0.f;
+      Chunk<T>::unpack(gam.c[0], w);
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const int heads = g ? a.heads - a.heads_q : a.heads_q, h0 = g ? a.heads_q : 0;
-      float g0[V], g1[V];
-      load_chunk(static_cast<const T*>(a.gamma) + g * a.dim + c0 * V, has0 && heads, g0);
-      load_chunk(static_cast<const T*>(a.gamma) + g * a.dim + c1 * V, has1 && heads, g1);
-      for (int r = threadIdx.x / G; r < n * heads; r += kThreads / G) {
-        const int k = r / heads, h = h0 + r - k * heads;
-        const T* src = static_cast<const T*>(a.x) + tok[k].x + h * a.xs[2];
-        const T* grad = static_cast<const T*>(a.dy) + tok[k].g + h * a.gs[2];
-        float u[V], v[V], p[V], q[V];
-        load_chunk(src + c0 * V, has0, u);
-        load_chunk(src + c1 * V, has1, v);
-        load_chunk(grad + c0 * V, has0, p);
-        load_chunk(grad + c1 * V, has1, q);
-        const float rstd = centre<G>(u, v, has0, has1, inv_dim, a.eps);
-        if (a.pairs) turn(p, q, cs + k * a.pairs, c0, c1, rotated, a.interleaved);
-        float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          u[e] *= rstd; v[e] *= rstd;
-          dgam[g][0][e] += p[e] * u[e]; dgam[g][1][e] += q[e] * v[e];
-          dbet[g][0][e] += p[e]; dbet[g][1][e] += q[e];
-          p[e] *= g0[e]; q[e] *= g1[e];
-          s1 += p[e] + q[e];
-          s2 += p[e] * u[e] + q[e] * v[e];
-        }
-        const float m1 = group_sum<G>(s1) * inv_dim, m2 = group_sum<G>(s2) * inv_dim;
-#pragma unroll
-        for (int e = 0; e < V; ++e) { u[e] = (p[e] - m1 - u[e] * m2) * rstd; v[e] = (q[e] - m1 - v[e] * m2) * rstd; }
-        T* dst = static_cast<T*>(a.out) + tok[k].o + h * a.os[2];
-        if (has0) *reinterpret_cast<u32x4*>(dst + c0 * V) = Chunk<T>::pack(u);
-        if (has1) *reinterpret_cast<u32x4*>(dst + c1 * V) = Chunk<T>::pack(v);
+      for (int e = 0; e < V; ++e) {
+        u[e] *= rstd;
+        dgam[0][e] += p[e] * u[e];
+        dbet[0][e] += p[e];
+        p[e] *= w[e];
+        s1 += p[e];
+        s2 += p[e] * u[e];
       }
+      Chunk<T>::unpack(gam.c[1], w);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        v[e] *= rstd;
+        dgam[1][e] += q[e] * v[e];
+        dbet[1][e] += q[e];
+        q[e] *= w[e];
+        s1 += q[e];
+        s2 += q[e] * v[e];
+      }
+      const float m1 = group_sum<G>(s1) * inv_dim, m2 = group_sum<G>(s2) * inv_dim;
+#pragma unroll
+      for (int e = 0; e < V; ++e) { u[e] = (p[e] - m1 - u[e] * m2) * rstd; v[e] = (q[e] - m1 - v[e] * m2) * rstd; }
+      Pair out;
+      out.c[0] = Chunk<T>::pack(u);
+      out.c[1] = Chunk<T>::pack(v);
+      store_pair(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], out, c0, c1, has0, has1);
     }
   }
-  // [lane groups][2][dim] floats of one group of heads at a time, added up in lane-group order
+  // [lane groups][2][dim] floats.  A column's lane groups are added up by as many threads as there are columns for, each a stretch of
+  // them in order, and the stretches in order.
   float* sums = reinterpret_cast<float*>(lds);
-  const int width = (a.heads > a.heads_q ? 2 : 1) * a.dim, slot = threadIdx.x / G;
+  __shared__ float part[kThreads];
+  const int columns = 2 * a.dim, width = (int)gridDim.y * a.dim, slot = threadIdx.x / G;
+  int stretches = 1;
+  while (stretches < S && 2 * stretches * columns <= kThreads) stretches *= 2;
+  const int per = S / stretches;
+  __syncthreads();
+  float* mine = sums + slot * columns;
 #pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    if (g && a.heads == a.heads_q) break;   // uniform
-    __syncthreads();
-    float* mine = sums + slot * 2 * a.dim;
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      if (has0) { mine[c0 * V + e] = dgam[g][0][e]; mine[a.dim + c0 * V + e] = dbet[g][0][e]; }
-      if (has1) { mine[c1 * V + e] = dgam[g][1][e]; mine[a.dim + c1 * V + e] = dbet[g][1][e]; }
-    }
-    __syncthreads();
-    for (int c = threadIdx.x; c < 2 * a.dim; c += kThreads) {
+  for (int e = 0; e < V; ++e) {
+    if (has0) { mine[c0 * V + e] = dgam[0][e]; mine[a.dim + c0 * V + e] = dbet[0][e]; }
+    if (has1) { mine[c1 * V + e] = dgam[1][e]; mine[a.dim + c1 * V + e] = dbet[1][e]; }
+  }
+  __syncthreads();
+  auto file = [&](int c, float s) {
+    const int which = c >= a.dim;
+    a.partial[((size_t)blockIdx.x * 2 + which) * width + g * a.dim + c - which * a.dim] = s;
+  };
+  if (stretches == 1) {
+    for (int c = threadIdx.x; c < columns; c += kThreads) {
       float s = 0.f;
-      for (int i = 0; i < kThreads / G; ++i) s += sums[i * 2 * a.dim + c];
-      const int which = c >= a.dim;
-      a.partial[((size_t)blockIdx.x * 2 + which) * width + g * a.dim + c - which * a.dim] = s;
+#pragma unroll 8
+      for (int i = 0; i < S; ++i) s += sums[i * columns + c];
+      file(c, s);
+    }
+  } else {
+    const int c = threadIdx.x % columns, stretch = threadIdx.x / columns;
+    float s = 0.f;
+    if (stretch < stretches) {
+#pragma unroll 8
+      for (int i = 0; i < per; ++i) s += sums[(stretch * per + i) * columns + c];
+    }
+    part[threadIdx.x] = s;
+    __syncthreads();
+    if ((int)threadIdx.x < columns) {
+      for (int i = 1; i < stretches; ++i) s += part[i * columns + threadIdx.x];
+      file(threadIdx.x, s);
     }
   }
 }
@@ -408,80 +479,67 @@ __global__ __launch_bounds__(kThreads) void heads_norm_backward_any_kernel(Args 
   Places at;
   at.init(lane, a.dim, a.pairs, a.interleaved);
   const float inv_dim = 1.f / (float)a.dim;
-  Row dgam[2], dbet[2];
-#pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    each(at, dgam[g], dgam[g], [](float& v, float, bool) { v = 0.f; });
-    each(at, dbet[g], dbet[g], [](float& v, float, bool) { v = 0.f; });
-  }
-  for (unsigned first = blockIdx.x * (unsigned)a.tokens_per_block; first < (unsigned)a.tokens; first += gridDim.x * (unsigned)a.tokens_per_block) {
-    const int n = min(a.tokens_per_block, a.tokens - (int)first);
+  const int g = blockIdx.y, heads = g ? a.heads - a.heads_q : a.heads_q, h0 = g ? a.heads_q : 0, per_block = g ? a.tokens_per_block_k : a.tokens_per_block;
+  Row dgam, dbet, gam;
+  each(at, dgam, dgam, [](float& v, float, bool) { v = 0.f; });
+  each(at, dbet, dbet, [](float& v, float, bool) { v = 0.f; });
+  load_row(static_cast<const T*>(a.gamma) + g * a.dim, at, gam);
+  for (unsigned first = blockIdx.x * (unsigned)per_block; first < (unsigned)a.tokens; first += gridDim.x * (unsigned)per_block) {
+    const int n = min(per_block, a.tokens - (int)first);
     __syncthreads();
     load_tokens(a, first, n, tok, cs);
     __syncthreads();
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const int heads = g ? a.heads - a.heads_q : a.heads_q, h0 = g ? a.heads_q : 0;
-      if (heads == 0) continue;   // uniform
-      Row gam;
-      load_row(static_cast<const T*>(a.gamma) + g * a.dim, at, gam);
-      for (int r = wave; r < n * heads; r += kThreads / 64) {
-        const int k = r / heads, h = h0 + r - k * heads;
-        Row x, d;
-        load_row(static_cast<const T*>(a.x) + tok[k].x + h * a.xs[2], at, x);
-        load_row(static_cast<const T*>(a.dy) + tok[k].g + h * a.gs[2], at, d);
-        const float rstd = centre_row(at, x, inv_dim, a.eps);
-        if (a.pairs) turn_row(d, at, cs + k * a.pairs, lane);
-        each(at, x, x, [&](float& v, float, bool) { v *= rstd; });
-        each(at, dbet[g], d, [](float& s, float v, bool) { s += v; });
-        Row dh = d;
-        each(at, dh, x, [](float& v, float xh, bool) { v *= xh; });
-        each(at, dgam[g], dh, [](float& s, float v, bool) { s += v; });
-        each(at, d, gam, [](float& v, float w, bool) { v *= w; });
-        float s1 = 0.f, s2 = 0.f;
-        each(at, d, x, [&](float& v, float xh, bool) { s1 += v; s2 += v * xh; });
-        const float m1 = group_sum<64>(s1) * inv_dim, m2 = group_sum<64>(s2) * inv_dim;
-        each(at, d, x, [&](float& v, float xh, bool) { v = (v - m1 - xh * m2) * rstd; });
-        store_row(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], at, d);
-      }
+    for (int r = wave; r < n * heads; r += kThreads / 64) {
+      const int k = r / heads, h = h0 + r - k * heads;
+      Row x, d;
+      load_row(static_cast<const T*>(a.x) + tok[k].x + h * a.xs[2], at, x);
+      load_row(static_cast<const T*>(a.dy) + tok[k].g + h * a.gs[2], at, d);
+      const float rstd = centre_row(at, x, inv_dim, a.eps);
+      if (a.pairs) turn_row(d, at, cs + k * a.pairs, lane);
+      each(at, x, x, [&](float& v, float, bool) { v *= rstd; });
+      each(at, dbet, d, [](float& s, float v, bool) { s += v; });
+      Row dh = d;
+      each(at, dh, x, [](float& v, float xh, bool) { v *= xh; });
+      each(at, dgam, dh, [](float& s, float v, bool) { s += v; });
+      each(at, d, gam, [](float& v, float w, bool) { v *= w; });
+      float s1 = 0.f, s2 = 0.f;
+      each(at, d, x, [&](float& v, float xh, bool) { s1 += v; s2 += v * xh; });
+      const float m1 = group_sum<64>(s1) * inv_dim, m2 = group_sum<64>(s2) * inv_dim;
+      each(at, d, x, [&](float& v, float xh, bool) { v = (v - m1 - xh * m2) * rstd; });
+      store_row(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], at, d);
     }
   }
   float* sums = reinterpret_cast<float*>(lds);   // [4 wavefronts][2][dim]
-  const int width = (a.heads > a.heads_q ? 2 : 1) * a.dim;
-#pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    if (g && a.heads == a.heads_q) break;   // uniform
-    __syncthreads();
-    store_row(sums + wave * 2 * a.dim, at, dgam[g]);
-    store_row(sums + wave * 2 * a.dim + a.dim, at, dbet[g]);
-    __syncthreads();
-    for (int c = threadIdx.x; c < 2 * a.dim; c += kThreads) {
-      const int which = c >= a.dim;
-      a.partial[((size_t)blockIdx.x * 2 + which) * width + g * a.dim + c - which * a.dim] =
-          ((sums[c] + sums[2 * a.dim + c]) + sums[4 * a.dim + c]) + sums[6 * a.dim + c];
-    }
+  const int width = (int)gridDim.y * a.dim;
+  __syncthreads();
+  store_row(sums + wave * 2 * a.dim, at, dgam);
+  store_row(sums + wave * 2 * a.dim + a.dim, at, dbet);
+  __syncthreads();
+  for (int c = threadIdx.x; c < 2 * a.dim; c += kThreads) {
+    const int which = c >= a.dim;
+    a.partial[((size_t)blockIdx.x * 2 + which) * width + g * a.dim + c - which * a.dim] =
+        ((sums[c] + sums[2 * a.dim + c]) + sums[4 * a.dim + c]) + sums[6 * a.dim + c];
   }
 }
 
 struct Route {
   int lanes = 0;             // lanes a row of the kernels of whole chunks, 0: the general kernels
-  int tokens_per_block = 1;
+  int tokens_per_block = 1, tokens_per_block_k = 1;
   long long blocks = 0;
+  int kinds = 1;             // blockIdx.y: queries, keys (backward with norm)
   size_t lds = 0;
 };
 
-// Blocks of tokens so that a launch has some 2048 of them, or as many as there are tokens; a backward pass that adds up weight gradients keeps
-// at most 1024 workgroups, which walk over the blocks.
-constexpr long long kBlocksWanted = 2048;
-constexpr long long kBackwardBlocks = 1024;
+// Tokens of a workgroup: so many that its rows make four rounds of its lanes (three in the backward pass with norm), which is when waiting for
+// the angles and the first rows stops to count, as long as 1024 workgroups (256 with norm backward) are left.  16389 tokens of 32 heads of 128: 53 us with
+// 4 tokens, 60 with 8; 8192 of 24 heads of 64: 10.5 with 8, 12.0 with 4 (one round and a half).
+// A backward pass with norm takes at most 512 workgroups a kind of head, which walk over the blocks and keep their sums: 16384 tokens of 32 heads of
+// 128: 91 us, with 256 122, with 1024 98; and the 512 partial rows take 4 us to add up.
+constexpr long long kBackwardBlocks = 512;
 
 Route route_of(const HeadsProblem& q, bool sums) {
   Route r;
   const long long tokens = (long long)q.batch * q.seq;
-  long long per = tokens / kBlocksWanted;
-  r.tokens_per_block = (int)std::min<long long>(std::max<long long>(per, 1), kMaxTokensPerBlock);
-  r.blocks = (tokens + r.tokens_per_block - 1) / r.tokens_per_block;
-  if (sums) r.blocks = std::min(r.blocks, kBackwardBlocks);
   const int v = q.dtype == DType::BF16 ? 8 : 4;
   auto whole = [&](const long long (&s)[3]) { return s[0] % v == 0 && s[1] % v == 0 && s[2] % v == 0; };
   const bool strides = whole(q.x_stride) && whole(q.out_stride) && (!q.dy || whole(q.dy_stride));
@@ -491,8 +549,20 @@ Route route_of(const HeadsProblem& q, bool sums) {
     r.lanes = 1;
     while (r.lanes * 2 * v < q.head_dim) r.lanes *= 2;
   }
-  r.lds = sizeof(Token) * kMaxTokensPerBlock + sizeof(float2) * (size_t)r.tokens_per_block * q.pairs;
-  if (sums) r.lds = std::max(r.lds, (size_t)(r.lanes ? kThreads / r.lanes : 4) * 2 * q.head_dim * sizeof(float));
+  const int at_once = r.lanes ? kThreads / r.lanes : kThreads / 64;   // rows a workgroup works on at a time
+  auto tokens_for = [&](int heads) {
+    const long long want = ((long long)(sums ? 3 : 4) * at_once + heads - 1) / heads;
+    return (int)std::max<long long>(1, std::min<long long>({want, kMaxTokensPerBlock, tokens / (sums ? 256 : 1024)}));
+  };
+  r.tokens_per_block = tokens_for(sums ? q.heads_q : q.heads_q + q.heads_k);
+  if (sums && q.heads_k) r.tokens_per_block_k = tokens_for(q.heads_k);
+  r.blocks = (tokens + r.tokens_per_block - 1) / r.tokens_per_block;
+  if (sums) {
+    r.blocks = std::min(r.blocks, kBackwardBlocks);
+    r.kinds = q.heads_k ? 2 : 1;
+  }
+  r.lds = sizeof(Token) * kMaxTokensPerBlock + sizeof(float2) * (size_t)std::max(r.tokens_per_block, r.tokens_per_block_k) * q.pairs;
+  if (sums) r.lds = std::max(r.lds, (size_t)at_once * 2 * q.head_dim * sizeof(float));
   return r;
 }
 
@@ -503,7 +573,7 @@ Args args_of(const HeadsProblem& q, const Route& r, bool inverse) {
   for (int i = 0; i < 3; ++i) { a.xs[i] = q.x_stride[i]; a.gs[i] = q.dy_stride[i]; a.os[i] = q.out_stride[i]; }
   a.tokens = q.batch * q.seq;
   a.seq = q.seq; a.heads_q = q.heads_q; a.heads = q.heads_q + q.heads_k; a.dim = q.head_dim;
-  a.pairs = q.pairs; a.interleaved = q.pairs ? q.interleaved : 0; a.norm = q.norm; a.inverse = inverse; a.tokens_per_block = r.tokens_per_block;
+  a.pairs = q.pairs; a.interleaved = q.pairs ? q.interleaved : 0; a.norm = q.norm; a.inverse = inverse; a.tokens_per_block = r.tokens_per_block; a.tokens_per_block_k = r.tokens_per_block_k;
   a.eps = q.eps;
   for (int j = 0; j < q.pairs; ++j) { a.axis[j] = (uint8_t)q.axis[j]; a.turns[j] = q.freq[j] / (2.0 * M_PI); }
   return a;
@@ -513,7 +583,7 @@ template <typename F>
 hipError_t launch(F* kernel, const Route& r, const Args& a, hipStream_t s) {
   if (r.lds > 64 * 1024)
     if (hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kernel), r.lds); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)r.blocks), dim3(kThreads), r.lds, s, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)r.blocks, (unsigned)r.kinds), dim3(kThreads), r.lds, s, a);
   return hipGetLastError();
 }
 
