@@ -45,14 +45,14 @@ struct Matrix {
   void* w;                 // first element of the matrix in its parameter
   const float* u;          // [rows, cols] dense
   const double* partial;   // [parts] sums of u^2
-  int parts, rows, cols, bf16, vector;   // vector: 8 entries of a row are whole 16-byte pieces
+  int parts, rows, cols, vector;   // vector: 8 entries of a row are whole 16-byte pieces
   float keep, step, eps;   // w = keep * w - step * X
 };
 
 // ---- elementwise half ---------------------------------------------------------------------------------------------
 
 constexpr int kMaxTensors = 16;
-constexpr int kPiece = 2048;              // elements a workgroup takes at a time
+constexpr int kPiece = 1024;              // elements a workgroup takes at a time
 constexpr int kMaxParts = 256;            // workgroups of one matrix
 
 struct Tensor {
@@ -75,14 +75,96 @@ struct Table {
 
 __device__ __forceinline__ float bf(uint16_t v) { return __uint_as_float(((uint32_t)v) << 16); }
 
+template <bool MATRIX>
 __device__ __forceinline__ void step_element(const Table& tab, const Tensor& t, float g, float& m, float& v, float& w, float& u) {
-  if (t.u) {
+  if constexpr (MATRIX) {
     m = tab.momentum * m + g;
     u = tab.nesterov ? g + tab.momentum * m : m;
   } else {
     m = tab.beta1 * m + tab.new1 * g;
     v = tab.beta2 * v + tab.new2 * (g * g);
     w = w * t.keep - t.rate * ((m * tab.inv_c1) / (sqrtf(v * tab.inv_c2) + tab.adam_eps));
+  }
+}
+
+// Four elements of a thread, all of their loads requested before the first is used.  C gradients, MATRIX: momentum and u, otherwise AdamW.
+template <int C, bool MATRIX>
+__device__ __forceinline__ void step_vector(const Table& tab, const Tensor& t, long long e0, float inv, double& sq) {
+  f32x4 x[C], v = {}, w = {};
+#pragma unroll
+  for (int j = 0; j < C; ++j) x[j] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(t.g[j] + e0));   // read once
+  f32x4 m = *reinterpret_cast<const f32x4*>(t.m + e0);
+  uint2 wb = {};
+  if constexpr (!MATRIX) {
+    v = *reinterpret_cast<const f32x4*>(t.v + e0);
+    if (t.bf16) wb = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(t.w) + e0);
+    else w = *reinterpret_cast<const f32x4*>(static_cast<const float*>(t.w) + e0);
+  }
+  f32x4 g = {0.f, 0.f, 0.f, 0.f}, u = {};
+#pragma unroll
+  for (int j = 0; j < C; ++j) g += x[j];   // workers added in the order given
+  if (!MATRIX && t.bf16) w = f32x4{__uint_as_float(wb.x << 16), __uint_as_float(wb.x & 0xFFFF0000u), __uint_as_float(wb.y << 16), __uint_as_float(wb.y & 0xFFFF0000u)};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float me = m[e], ve = v[e], we = w[e], ue = 0.f;
+    step_element<MATRIX>(tab, t, g[e] * inv, me, ve, we, ue);
+    m[e] = me; v[e] = ve; w[e] = we; u[e] = ue;
+  }
+  *reinterpret_cast<f32x4*>(t.m + e0) = m;
+  if constexpr (MATRIX) {
+    *reinterpret_cast<f32x4*>(t.u + e0) = u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sq += (double)u[e] * (double)u[e];
+  } else {
+    *reinterpret_cast<f32x4*>(t.v + e0) = v;
+    if (t.bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(t.w) + e0) = uint2{bf16_pack2(w[0], w[1]), bf16_pack2(w[2], w[3])};
+    else *reinterpret_cast<f32x4*>(static_cast<float*>(t.w) + e0) = w;
+  }
+}
+// The same element by element: any number of elements, any alignment.
+template <bool MATRIX>
+__device__ __forceinline__ void step_scalar(const Table& tab, const Tensor& t, long long e0, long long end, float inv, double& sq) {
+  const int live = (int)min(end - e0, 4ll);
+  for (int e = 0; e < live; ++e) {
+    const long long at = e0 + e;
+    float g = 0.f, m = t.m[at], v = 0.f, w = 0.f, u = 0.f;
+    for (int j = 0; j < t.count; ++j) g += t.g[j][at];
+    if (!MATRIX) {
+      v = t.v[at];
+      w = t.bf16 ? bf(static_cast<const uint16_t*>(t.w)[at]) : static_cast<const float*>(t.w)[at];
+    }
+    step_element<MATRIX>(tab, t, g * inv, m, v, w, u);
+    t.m[at] = m;
+    if (MATRIX) {
+      t.u[at] = u;
+      sq += (double)u * (double)u;
+    } else {
+      t.v[at] = v;
+      if (t.bf16) static_cast<uint16_t*>(t.w)[at] = bf16_round(w);
+      else static_cast<float*>(t.w)[at] = w;
+    }
+  }
+}
+template <int C, bool MATRIX>
+__device__ __forceinline__ void step_range(const Table& tab, const Tensor& t, long long begin, long long end, double& sq) {
+  const float inv = 1.f / (float)t.count;
+  for (long long e0 = begin + threadIdx.x * 4; e0 < end; e0 += kThreads * 4) {
+    if constexpr (C > 0) step_vector<C, MATRIX>(tab, t, e0, inv, sq);
+    else step_scalar<MATRIX>(tab, t, e0, end, inv, sq);
+  }
+}
+template <bool MATRIX>
+__device__ __forceinline__ void step_tensor(const Table& tab, const Tensor& t, long long begin, long long end, double& sq) {
+  switch (t.vector ? t.count : 0) {   // uniform over the workgroup
+    case 1: step_range<1, MATRIX>(tab, t, begin, end, sq); return;
+    case 2: step_range<2, MATRIX>(tab, t, begin, end, sq); return;
+    case 3: step_range<3, MATRIX>(tab, t, begin, end, sq); return;
+    case 4: step_range<4, MATRIX>(tab, t, begin, end, sq); return;
+    case 5: step_range<5, MATRIX>(tab, t, begin, end, sq); return;
+    case 6: step_range<6, MATRIX>(tab, t, begin, end, sq); return;
+    case 7: step_range<7, MATRIX>(tab, t, begin, end, sq); return;
+    case 8: step_range<8, MATRIX>(tab, t, begin, end, sq); return;
+    default: step_range<0, MATRIX>(tab, t, begin, end, sq);
   }
 }
 
@@ -95,67 +177,9 @@ __global__ __launch_bounds__(kThreads) void update_kernel(Table tab) {
   const int mat = local / t.parts, part = local - mat * t.parts;
   const long long base = mat * t.numel;
   const long long begin = base + part * t.chunk, end = base + min(t.numel, (part + 1) * t.chunk);
-  const float inv = 1.f / (float)t.count;
   double sq = 0.0;
-  for (long long e0 = begin + threadIdx.x * 4; e0 < end; e0 += kThreads * 4) {
-    float g[4] = {0.f, 0.f, 0.f, 0.f}, m[4] = {}, v[4] = {}, w[4] = {}, u[4] = {};
-    const int live = (int)min(end - e0, 4ll);
-    if (t.vector) {
-      for (int j = 0; j < t.count; ++j) {
-        const f32x4 x = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(t.g[j] + e0));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) g[e] += x[e];
-      }
-      const f32x4 mm = *reinterpret_cast<const f32x4*>(t.m + e0);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) m[e] = mm[e];
-      if (!t.u) {
-        const f32x4 vv = *reinterpret_cast<const f32x4*>(t.v + e0);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = vv[e];
-        if (t.bf16) {
-          const uint2 b = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(t.w) + e0);
-          w[0] = __uint_as_float(b.x << 16); w[1] = __uint_as_float(b.x & 0xFFFF0000u);
-          w[2] = __uint_as_float(b.y << 16); w[3] = __uint_as_float(b.y & 0xFFFF0000u);
-        } else {
-          const f32x4 ww = *reinterpret_cast<const f32x4*>(static_cast<const float*>(t.w) + e0);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = ww[e];
-        }
-      }
-    } else {
-      for (int j = 0; j < t.count; ++j)
-        for (int e = 0; e < live; ++e) g[e] += t.g[j][e0 + e];
-      for (int e = 0; e < live; ++e) m[e] = t.m[e0 + e];
-      if (!t.u)
-        for (int e = 0; e < live; ++e) {
-          v[e] = t.v[e0 + e];
-          w[e] = t.bf16 ? bf(static_cast<const uint16_t*>(t.w)[e0 + e]) : static_cast<const float*>(t.w)[e0 + e];
-        }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      step_element(tab, t, g[e] * inv, m[e], v[e], w[e], u[e]);
-      if (e < live) sq += (double)u[e] * (double)u[e];
-    }
-    if (t.vector) {
-      *reinterpret_cast<f32x4*>(t.m + e0) = f32x4{m[0], m[1], m[2], m[3]};
-      if (t.u) *reinterpret_cast<f32x4*>(t.u + e0) = f32x4{u[0], u[1], u[2], u[3]};
-      else {
-        *reinterpret_cast<f32x4*>(t.v + e0) = f32x4{v[0], v[1], v[2], v[3]};
-        if (t.bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(t.w) + e0) = uint2{bf16_pack2(w[0], w[1]), bf16_pack2(w[2], w[3])};
-        else *reinterpret_cast<f32x4*>(static_cast<float*>(t.w) + e0) = f32x4{w[0], w[1], w[2], w[3]};
-      }
-    } else {
-      for (int e = 0; e < live; ++e) {
-        t.m[e0 + e] = m[e];
-        if (t.u) { t.u[e0 + e] = u[e]; continue; }
-        t.v[e0 + e] = v[e];
-        if (t.bf16) static_cast<uint16_t*>(t.w)[e0 + e] = bf16_round(w[e]);
-        else static_cast<float*>(t.w)[e0 + e] = w[e];
-      }
-    }
-  }
+  if (t.u) step_tensor<true>(tab, t, begin, end, sq);
+  else step_tensor<false>(tab, t, begin, end, sq);
   if (!t.u) return;   // uniform over the workgroup
   __shared__ double sums[kThreads / 64];
 #pragma unroll
@@ -166,7 +190,7 @@ __global__ __launch_bounds__(kThreads) void update_kernel(Table tab) {
     t.partial[(long long)mat * t.parts + part] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     if (part == 0)
       t.out[mat] = Matrix{t.bf16 ? (void*)(static_cast<uint16_t*>(t.w) + base) : (void*)(static_cast<float*>(t.w) + base), t.u + base,
-                          t.partial + (long long)mat * t.parts, t.parts, t.rows, t.cols, t.bf16, t.vector && t.cols % 8 == 0, t.keep, t.step, tab.ns_eps};
+                          t.partial + (long long)mat * t.parts, t.parts, t.rows, t.cols, t.vector && t.cols % 8 == 0, t.keep, t.step, tab.ns_eps};
   }
 }
 
@@ -271,20 +295,30 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(Groups groups) {
   }
 }
 
-// w = keep * w - step * X for 8 entries of one row of the parameter; v: sigma X.
-__device__ __forceinline__ void apply8(const Matrix& d, float inv_sigma, const float (&v)[8], int row, int col) {
+// 8 entries of one row of the parameter (bfloat16 with one plane, float32 with two) as they are before the step, requested ahead where they are whole
+// 16-byte pieces.
+template <int PLANES> struct Entries { u32x4 c[PLANES]; };
+__device__ __forceinline__ bool whole8(const Matrix& d, int row, int col) { return d.vector && row < d.rows && col + 8 <= d.cols; }
+template <int PLANES>
+__device__ __forceinline__ void request8(const Matrix& d, int row, int col, Entries<PLANES>& to) {
+  if (!whole8(d, row, col)) return;
+  const char* w = static_cast<const char*>(d.w) + ((size_t)row * d.cols + col) * (PLANES == 2 ? 4 : 2);
+#pragma unroll
+  for (int h = 0; h < PLANES; ++h) to.c[h] = *reinterpret_cast<const u32x4*>(w + 16 * h);
+}
+// w = keep * w - step * X; v: sigma X.
+template <int PLANES>
+__device__ __forceinline__ void apply8(const Matrix& d, float inv_sigma, const float (&v)[8], int row, int col, const Entries<PLANES>& old) {
   if (row >= d.rows || col >= d.cols) return;
   const float step = d.step * inv_sigma;
   const size_t at = (size_t)row * d.cols + col;
-  const bool whole = col + 8 <= d.cols && d.vector;
-  if (d.bf16) {
+  if constexpr (PLANES == 1) {
     uint16_t* w = static_cast<uint16_t*>(d.w) + at;
-    if (whole) {
-      const u32x4 old = *reinterpret_cast<const u32x4*>(w);
+    if (whole8(d, row, col)) {
       u32x4 out;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        out[e] = bf16_pack2(d.keep * __uint_as_float(old[e] << 16) - step * v[2 * e], d.keep * __uint_as_float(old[e] & 0xFFFF0000u) - step * v[2 * e + 1]);
+        out[e] = bf16_pack2(d.keep * __uint_as_float(old.c[0][e] << 16) - step * v[2 * e], d.keep * __uint_as_float(old.c[0][e] & 0xFFFF0000u) - step * v[2 * e + 1]);
       *reinterpret_cast<u32x4*>(w) = out;
     } else {
 #pragma unroll
@@ -293,13 +327,13 @@ __device__ __forceinline__ void apply8(const Matrix& d, float inv_sigma, const f
     }
   } else {
     float* w = static_cast<float*>(d.w) + at;
-    if (whole) {
+    if (whole8(d, row, col)) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        f32x4 old = *reinterpret_cast<const f32x4*>(w + 4 * h);
+        f32x4 out;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) old[e] = d.keep * old[e] - step * v[4 * h + e];
-        *reinterpret_cast<f32x4*>(w + 4 * h) = old;
+        for (int e = 0; e < 4; ++e) out[e] = d.keep * __uint_as_float(old.c[h][e]) - step * v[4 * h + e];
+        *reinterpret_cast<f32x4*>(w + 4 * h) = out;
       }
     } else {
 #pragma unroll
@@ -341,6 +375,34 @@ struct Panel {
 
 enum Mode { kGram = 0, kPoly = 1, kUpdate = 2, kFinal = 3 };
 
+// Row and column of a matrix's tile number `tile`: those on and below the diagonal of a symmetric result, or all, down the columns.
+template <int MODE>
+__device__ __forceinline__ void place_tile(int tile, int tiles_m, int& ti, int& tj) {
+  if constexpr (MODE == kGram || MODE == kPoly) {
+    ti = (int)((sqrtf(8.f * (float)tile + 1.f) - 1.f) * 0.5f);
+    while (ti * (ti + 1) / 2 > tile) --ti;
+    while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
+    tj = tile - ti * (ti + 1) / 2;
+  } else {
+    tj = tile / tiles_m;
+    ti = tile - tj * tiles_m;
+  }
+}
+
+// From the sums of a product to what is stored, for 8 entries; s: kPoly's entries of A; diagonal: which of the 8 lies on the diagonal, if any.
+template <int MODE, int PLANES>
+__device__ __forceinline__ void finish8(float (&v)[8], float inv_sigma, const u32x4 (&s)[PLANES], int diagonal) {
+  const float by = MODE == kGram ? kTau * inv_sigma * inv_sigma : MODE == kPoly ? kC / kTau : 1.f / kTau;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] *= by;
+  if constexpr (MODE == kPoly) {
+    float f[8];
+    join8<PLANES>(s, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += kB * f[e] + (e == diagonal ? kA * kTau : 0.f);
+  }
+}
+
 // kGram: A = X X^T.  kPoly: B = a I + b A + c A A.  kUpdate: X' = B X.  kFinal: the same, applied to the parameter.
 // (a I inside B, so that the update reads nothing but the product's operands: X behind the tile loop once more was 200 MB of 24 matrices of 1024 x 4096, and
 // its latency stood between the loop and the stores.)
@@ -369,16 +431,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(Groups 
   int mat, tile;
   const Group& g = group_of(groups, xcd_tile(blockIdx.x, gridDim.x), mat, tile);
   int ti, tj;
-  if constexpr (MODE == kGram || MODE == kPoly) {   // on and below the diagonal
-    ti = (int)((sqrtf(8.f * (float)tile + 1.f) - 1.f) * 0.5f);
-    while (ti * (ti + 1) / 2 > tile) --ti;
-    while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
-    tj = tile - ti * (ti + 1) / 2;
-  } else {
-    const int tiles_m = g.mp / BT;
-    tj = tile / tiles_m;
-    ti = tile - tj * tiles_m;
-  }
+  place_tile<MODE>(tile, g.mp / BT, ti, tj);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % WAVES_M, wn = wave / WAVES_M;
   const size_t plane_x = (size_t)g.mp * g.np, plane_a = (size_t)g.mp * g.mp;
@@ -444,19 +497,37 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(Groups 
     else if constexpr (R < kReads) fq[S][R - PLANES * TM] = ReaderQ::template read<(R - PLANES * TM) % TN, KG>(where.q[(R - PLANES * TM) / TN]);
   };
 
-  // kPoly: the entries of A that 32 rows of the wave's tile are combined with, requested one strip ahead, the first here
-  constexpr int LD = WN + 4, kUnits = WN / 16;         // units of 8 columns of a lane
+  // What 32 rows of the wave's tile are combined with - kPoly: entries of A, kFinal: the parameter's - is requested one strip ahead, the first here.
+  constexpr int LD = WN + 4, kUnits = WN / 16;         // units of 8 entries of a lane
+  const Matrix d = MODE == kFinal ? g.matrices[mat] : Matrix{};
+  const bool turn = MODE == kFinal ? d.rows > d.cols : ti != tj;   // a mirror image to write, or a tall parameter
   u32x4 held[2][kUnits][PLANES];
-  auto load_strip = [&](int i, u32x4 (&to)[kUnits][PLANES]) {
+  Entries<PLANES> old[2][kUnits];
+  // rows and columns of unit k of strip i: along the rows, and along the columns
+  auto unit = [&](int i, int k, int& row, int& col, int& r, int& c) {
+    r = (k * 64 + lane) / (WN / 8); c = (k * 64 + lane) % (WN / 8) * 8;
+    row = ti * BT + wm * WM + i * 32 + r; col = tj * BT + wn * WN + c;
+  };
+  auto turned = [&](int i, int k, int& row, int& col, int& r, int& c) {
+    c = k * 16 + (lane >> 2); r = (lane & 3) * 8;
+    row = tj * BT + wn * WN + c; col = ti * BT + wm * WM + i * 32 + r;
+  };
+  auto request = [&](int i) {
+    int row, col, r, c;
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-      const int unit = k * 64 + lane, r = unit / (WN / 8), c = (unit % (WN / 8)) * 8;
+      if constexpr (MODE == kPoly) {
+        unit(i, k, row, col, r, c);
 #pragma unroll
-      for (int pl = 0; pl < PLANES; ++pl)
-        to[k][pl] = *reinterpret_cast<const u32x4*>(a + pl * plane_a + (size_t)(ti * BT + wm * WM + i * 32 + r) * g.mp + tj * BT + wn * WN + c);
+        for (int pl = 0; pl < PLANES; ++pl) held[i & 1][k][pl] = *reinterpret_cast<const u32x4*>(a + pl * plane_a + (size_t)row * g.mp + col);
+      } else if constexpr (MODE == kFinal) {
+        if (turn) turned(i, k, row, col, r, c);
+        else unit(i, k, row, col, r, c);
+        request8<PLANES>(d, row, col, old[i & 1][k]);
+      }
     }
   };
-  if constexpr (MODE == kPoly) load_strip(0, held[0]);
+  request(0);
 #pragma unroll
   for (int t = 0; t < STAGES - 1; ++t)
 #pragma unroll
@@ -524,14 +595,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(Groups 
   // 16-byte pieces: first row by row, then, for a mirror image or a tall parameter, column by column from what the first left there.
   float* strip = reinterpret_cast<float*>(lds) + wave * (32 * LD);
   const float inv_sigma = 1.f / g.sigma;
-  const Matrix d = MODE == kFinal ? g.matrices[mat] : Matrix{};
-  const bool tall = d.rows > d.cols;
-  const bool turn = MODE == kFinal ? tall : ti != tj;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    const int row0 = ti * BT + wm * WM + i * 32, col0 = tj * BT + wn * WN;
-    if constexpr (MODE == kPoly)
-      if (i + 1 < TM) load_strip(i + 1, held[(i + 1) & 1]);
+    if (i + 1 < TM) request(i + 1);
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -540,26 +606,16 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(Groups 
     gemm_dma_detail::lanes_together();
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-      const int unit = k * 64 + lane, r = unit / (WN / 8), c = (unit % (WN / 8)) * 8;
+      int row, col, r, c;
+      unit(i, k, row, col, r, c);
       float* at_s = strip + r * LD + c;
       const f32x4 lo = *reinterpret_cast<const f32x4*>(at_s), hi = *reinterpret_cast<const f32x4*>(at_s + 4);
       float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (MODE == kGram) v[e] *= kTau * inv_sigma * inv_sigma;
-        else if constexpr (MODE == kPoly) v[e] *= kC / kTau;
-        else v[e] *= 1.f / kTau;
-      }
-      if constexpr (MODE == kPoly) {
-        float s[8];
-        join8<PLANES>(held[i & 1][k], s);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += kB * s[e] + (row0 + r == col0 + c + e ? kA * kTau : 0.f);
-      }
-      if constexpr (MODE == kGram) split8<PLANES>(v, a + (size_t)(row0 + r) * g.mp + col0 + c, plane_a);
-      else if constexpr (MODE == kPoly) split8<PLANES>(v, b + (size_t)(row0 + r) * g.mp + col0 + c, plane_a);
-      else if constexpr (MODE == kUpdate) split8<PLANES>(v, g.x[1] + mat * PLANES * plane_x + (size_t)(row0 + r) * g.np + col0 + c, plane_x);
-      else if (!turn) apply8(d, inv_sigma, v, row0 + r, col0 + c);
+      finish8<MODE, PLANES>(v, inv_sigma, held[i & 1][k], row - col);
+      if constexpr (MODE == kGram) split8<PLANES>(v, a + (size_t)row * g.mp + col, plane_a);
+      else if constexpr (MODE == kPoly) split8<PLANES>(v, b + (size_t)row * g.mp + col, plane_a);
+      else if constexpr (MODE == kUpdate) split8<PLANES>(v, g.x[1] + mat * PLANES * plane_x + (size_t)row * g.np + col, plane_x);
+      else if (!turn) apply8<PLANES>(d, inv_sigma, v, row, col, old[i & 1][k]);
       if (MODE != kUpdate && turn) {
         *reinterpret_cast<f32x4*>(at_s) = f32x4{v[0], v[1], v[2], v[3]};
         *reinterpret_cast<f32x4*>(at_s + 4) = f32x4{v[4], v[5], v[6], v[7]};
@@ -570,13 +626,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(Groups 
       if (turn) {   // uniform
 #pragma unroll
         for (int k = 0; k < kUnits; ++k) {
-          const int c = k * 16 + (lane >> 2), r = (lane & 3) * 8;
+          int row, col, r, c;
+          turned(i, k, row, col, r, c);
           float v[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = strip[(r + e) * LD + c];
-          if constexpr (MODE == kGram) split8<PLANES>(v, a + (size_t)(col0 + c) * g.mp + row0 + r, plane_a);
-          else if constexpr (MODE == kPoly) split8<PLANES>(v, b + (size_t)(col0 + c) * g.mp + row0 + r, plane_a);
-          else apply8(d, inv_sigma, v, col0 + c, row0 + r);
+          if constexpr (MODE == kGram) split8<PLANES>(v, a + (size_t)row * g.mp + col, plane_a);
+          else if constexpr (MODE == kPoly) split8<PLANES>(v, b + (size_t)row * g.mp + col, plane_a);
+          else apply8<PLANES>(d, inv_sigma, v, row, col, old[i & 1][k]);
         }
         gemm_dma_detail::lanes_together();
       }
@@ -584,19 +641,159 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(Groups 
   }
 }
 
+// The same products where there are few tiles and a product is a chain of latencies: tiles of 32 x 32, so that more CUs have one, whose k range
+// the four wavefronts share.  Each has a ring of its own and waits on its own loads only; their partial tiles are added up through LDS, in
+// wavefront order.  (One float32 matrix of 256 x 784: A = X X^T 10.1 us in tiles of 64 by four wavefronts in step.)
+template <int MODE, int PLANES, int SW>
+__global__ __launch_bounds__(kThreads) void small_product_kernel(Groups groups) {
+  constexpr int BT = 32, NW = 4, LD = BT + 4;
+  constexpr int kPanelBytes = BT * 128, kStageBytes = 2 * PLANES * kPanelBytes, kLoads = 2 * PLANES * (BT / 8);
+  static_assert((SW - 1) * kLoads < 64, "vmcnt range");
+  static_assert((size_t)NW * BT * LD * 4 <= (size_t)NW * SW * kStageBytes, "partial tiles fit in the rings");
+  constexpr Layout LQ = MODE == kGram || MODE == kPoly ? Layout::RowK : Layout::KRow;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  int mat, tile, ti, tj;
+  const Group& g = group_of(groups, xcd_tile(blockIdx.x, gridDim.x), mat, tile);
+  place_tile<MODE>(tile, g.mp / BT, ti, tj);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const size_t plane_x = (size_t)g.mp * g.np, plane_a = (size_t)g.mp * g.mp;
+  const _Float16* x = g.x[0] + mat * PLANES * plane_x;
+  _Float16* a = g.a + mat * PLANES * plane_a;
+  _Float16* b = g.b + mat * PLANES * plane_a;
+  const size_t plane_p = (MODE == kGram ? plane_x : plane_a) * 2, plane_q = (MODE == kPoly ? plane_a : plane_x) * 2;   // bytes
+  const int k_tiles = (MODE == kGram ? g.np : g.mp) / kTileK, per_wave = (k_tiles + NW - 1) / NW;
+  const int first = min(wave * per_wave, k_tiles), n = min(first + per_wave, k_tiles) - first;
+  char* ring = lds + wave * (SW * kStageBytes);
+  Panel<BT, Layout::RowK, 1> sp;
+  Panel<BT, LQ, 1> sq;
+  sp.init(MODE == kGram ? x : MODE == kPoly ? a : b, MODE == kGram ? g.np : g.mp, ti * BT, 0, lane);
+  sq.init(MODE == kPoly ? a : x, MODE == kPoly ? g.mp : g.np, tj * BT, 0, lane);
+  auto issue = [&](int t) {
+    char* stage = ring + (t % SW) * kStageBytes;
+#pragma unroll
+    for (int pl = 0; pl < PLANES; ++pl)
+#pragma unroll
+      for (int i = 0; i < BT / 8; ++i) {
+        sp.load(i, sp.base + (first + t) * sp.step + pl * plane_p, stage + pl * kPanelBytes, 0);
+        sq.load(i, sq.base + (first + t) * sq.step + pl * plane_q, stage + (PLANES + pl) * kPanelBytes, 0);
+      }
+  };
+  // what this thread's 8 entries are combined with (threads of the first two wavefronts)
+  const int r = (threadIdx.x & 127) >> 2, c = (threadIdx.x & 3) * 8;
+  const Matrix d = MODE == kFinal ? g.matrices[mat] : Matrix{};
+  const bool turn = MODE == kFinal ? d.rows > d.cols : ti != tj, finishes = threadIdx.x < 128;
+  u32x4 held[PLANES];
+  Entries<PLANES> old;
+  if (finishes) {
+    if constexpr (MODE == kPoly) {
+#pragma unroll
+      for (int pl = 0; pl < PLANES; ++pl) held[pl] = *reinterpret_cast<const u32x4*>(a + pl * plane_a + (size_t)(ti * BT + r) * g.mp + tj * BT + c);
+    } else if constexpr (MODE == kFinal) {
+      request8<PLANES>(d, (turn ? tj : ti) * BT + r, (turn ? ti : tj) * BT + c, old);
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < SW; ++s)
+    if (s < n) issue(s);
+  f32x16 acc, acc_lo;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = acc_lo[e] = 0.f;
+  using ReaderP = gemm_dma_detail::FragmentReader<BT, Layout::RowK, 1>;
+  using ReaderQ = gemm_dma_detail::FragmentReader<BT, LQ, 1>;
+  ReaderP reader_p;
+  ReaderQ reader_q;
+  reader_p.init(0, lane);
+  reader_q.init(0, lane);
+  for (int t = 0; t < n; ++t) {
+    asm volatile("" ::: "memory");
+    if (t + SW <= n) __builtin_amdgcn_s_waitcnt(gemm_dma_detail::waitcnt_imm((SW - 1) * kLoads, 15));
+    else __builtin_amdgcn_s_waitcnt(gemm_dma_detail::waitcnt_imm(0, 15));
+    asm volatile("" ::: "memory");
+    const uint32_t base = (uint32_t)(uintptr_t)(gemm_dma_detail::lds_ptr_t)(ring + (t % SW) * kStageBytes);
+    u32x4 fp[4 * PLANES], fq[4 * PLANES];
+    gemm_detail::static_for<PLANES>([&](auto pl_c) {
+      constexpr int pl = decltype(pl_c)::value;
+      uint32_t at_p[ReaderP::kN], at_q[ReaderQ::kN];
+      reader_p.at(base + pl * kPanelBytes, at_p);
+      reader_q.at(base + (PLANES + pl) * kPanelBytes, at_q);
+      gemm_detail::static_for<4>([&](auto kg) {
+        fp[pl * 4 + decltype(kg)::value] = ReaderP::template read<0, decltype(kg)::value>(at_p);
+        fq[pl * 4 + decltype(kg)::value] = ReaderQ::template read<0, decltype(kg)::value>(at_q);
+      });
+    });
+    gemm_dma_detail::fragments_ready(fp, fq);
+    if (t + SW < n) issue(t + SW);   // over the tile that is in registers now
+#pragma unroll
+    for (int kg = 0; kg < 4; ++kg) {
+      auto mfma = [&](const u32x4& qf, const u32x4& pf, f32x16& into) {
+        into = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, qf), __builtin_bit_cast(f16x8, pf), into, 0, 0, 0);
+      };
+      mfma(fq[kg], fp[kg], acc);
+      if constexpr (PLANES == 2) {
+        mfma(fq[4 + kg], fp[kg], acc_lo);
+        mfma(fq[kg], fp[4 + kg], acc_lo);
+      }
+    }
+  }
+  if constexpr (PLANES == 2) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] += acc_lo[e] * (1.f / kLoScale);
+  }
+  __syncthreads();   // every ring is dead
+  float* parts = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int e = 0; e < 16; e += 4)
+    *reinterpret_cast<f32x4*>(parts + wave * (BT * LD) + (lane & 31) * LD + 2 * e + 4 * (lane >> 5)) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+  __syncthreads();
+  const float inv_sigma = 1.f / g.sigma;
+  if (finishes) {
+    float* at_s = parts + r * LD + c;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = ((at_s[e] + at_s[BT * LD + e]) + at_s[2 * BT * LD + e]) + at_s[3 * BT * LD + e];
+    const int row = ti * BT + r, col = tj * BT + c;
+    finish8<MODE, PLANES>(v, inv_sigma, held, row - col);
+    if constexpr (MODE == kGram) split8<PLANES>(v, a + (size_t)row * g.mp + col, plane_a);
+    else if constexpr (MODE == kPoly) split8<PLANES>(v, b + (size_t)row * g.mp + col, plane_a);
+    else if constexpr (MODE == kUpdate) split8<PLANES>(v, g.x[1] + mat * PLANES * plane_x + (size_t)row * g.np + col, plane_x);
+    else if (!turn) apply8<PLANES>(d, inv_sigma, v, row, col, old);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) at_s[e] = v[e];
+  }
+  if constexpr (MODE != kUpdate) {
+    if (!turn) return;   // uniform over the workgroup
+    __syncthreads();
+    if (!finishes) return;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = parts[(c + e) * LD + r];
+    const int row = tj * BT + r, col = ti * BT + c;
+    if constexpr (MODE == kGram) split8<PLANES>(v, a + (size_t)row * g.mp + col, plane_a);
+    else if constexpr (MODE == kPoly) split8<PLANES>(v, b + (size_t)row * g.mp + col, plane_a);
+    else apply8<PLANES>(d, inv_sigma, v, row, col, old);
+  }
+}
+
 // ---- plan -----------------------------------------------------------------------------------------------------------
 
 // What a product of `count` matrices in tiles of `tile` takes, in us, from these kernels' times over 1 to 64 matrices of 64 x 64 to 4096 x 4096: rounds of
-// workgroups over the 256 CUs, each a start and an end (2 to 8 us) and so much for every 64 of k.  Tiles of 64 and of 256 have a CU to
+// workgroups over the 256 CUs, each a start and an end (2 to 8 us) and so much for every 64 of k, less where a round is alone.  Tiles of 64 and of 256 have a CU to
 // themselves (rings of 96 and 128 KB); those of 128 share one with another once there are more than CUs (24 products of 1024 x 4096 x 1024: 272 us so, 345 us
 // alone on a ring of four), and have it to themselves before (136 tiles over k = 2048: 26 against 23).  One float32 product of 1024 x 1024 x 1024: tiles
-// of 64 13 us, of 128 24; 16 of them: 175 and 112.  48 of 768 x 768 x 768: tiles of 128 62 us, of 256 53; their symmetric halves 44 and 53.
+// of 64 13 us, of 128 24; 16 of them: 175 and 112.  One of 256 x 256 x 784: tiles of 32 6.0 us, of 64 10.5; one bfloat16 product of 512 cubed 4.2 and 6.2, of 2048
+// cubed 80 and 55, and in tiles of 128 25.  48 of 768 x 768 x 768: tiles of 128 62 us, of 256 53; their symmetric halves 44 and 53.
 double product_cost(long long tiles, int tile, int planes, int k) {
   const double steps = k / 64;
   auto rounds = [&](int at_once) { return (double)((tiles + at_once - 1) / at_once); };
-  if (planes == 2) return tile == 64 ? rounds(256) * (2.0 + 0.56 * steps) : rounds(256) * (5.0 + 1.44 * steps);
-  if (tile == 64) return rounds(256) * (2.8 + 0.29 * steps);
-  if (tile == 128) return tiles <= 256 ? 5.0 + 0.6 * steps : rounds(512) * (6.0 + 1.0 * steps);
+  const bool alone = tiles <= 256;
+  if (planes == 2) {
+    if (tile == 32) return alone ? 3.6 + 0.16 * steps : rounds(256) * (3.2 + 0.26 * steps);
+    if (tile == 64) return alone ? 4.7 + 0.42 * steps : rounds(256) * (2.0 + 0.56 * steps);
+    return rounds(256) * (5.0 + 1.44 * steps);
+  }
+  if (tile == 32) return alone ? 2.8 + 0.09 * steps : rounds(512) * (2.0 + 0.24 * steps);
+  if (tile == 64) return alone ? 4.2 + 0.29 * steps : rounds(256) * (2.8 + 0.29 * steps);
+  if (tile == 128) return alone ? 5.0 + 0.6 * steps : rounds(512) * (6.0 + 1.0 * steps);
   return rounds(256) * (8.0 + 1.64 * steps);
 }
 
@@ -610,9 +807,9 @@ constexpr int largest_tile(int planes) { return planes == 2 ? 128 : 256; }
 // The cheapest tile among those that divide the padded sides, for all groups of a launch together.
 template <class Sizes>
 int pick_tile(int mode, int planes, int pad, const Sizes& groups, int n, double* cost = nullptr) {
-  int best = 64;
+  int best = 32;
   double least = 0.0;
-  for (int tile = 64; tile <= std::min(pad, largest_tile(planes)); tile *= 2) {
+  for (int tile = 32; tile <= std::min(pad, largest_tile(planes)); tile *= 2) {
     long long tiles = 0;
     int k = 0;
     for (int i = 0; i < n; ++i) {
@@ -620,7 +817,7 @@ int pick_tile(int mode, int planes, int pad, const Sizes& groups, int n, double*
       k = std::max(k, mode == kGram ? groups[i].np : groups[i].mp);
     }
     const double c = product_cost(tiles, tile, planes, k);
-    if (tile == 64 || c < least) { best = tile; least = c; }
+    if (tile == 32 || c < least) { best = tile; least = c; }
   }
   if (cost) *cost = least;
   return best;
@@ -766,10 +963,22 @@ int lay_out(Groups& t, F&& per_matrix) {
 }
 
 template <int MODE, int PLANES>
+hipError_t launch_small_product(const Groups& t, int blocks, hipStream_t s) {
+  constexpr int SW = 2;
+  auto* kernel = small_product_kernel<MODE, PLANES, SW>;
+  constexpr size_t lds = (size_t)4 * SW * 2 * PLANES * 32 * 128;
+  if (lds > 64 * 1024)
+    if (hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), lds, s, t);
+  return hipGetLastError();
+}
+
+template <int MODE, int PLANES>
 hipError_t product(Groups& t, int pad, hipStream_t s) {
   const int tile = pick_tile(MODE, PLANES, pad, t.g, t.n);
   const int blocks = lay_out(t, [&](const Group& g) { return tiles_of(MODE, g.mp, g.np, tile); });
   if (blocks < 0) return hipErrorInvalidValue;
+  if (tile == 32) return launch_small_product<MODE, PLANES>(t, blocks, s);
   if constexpr (PLANES == 1) {
     if (tile == 256) return launch_product<MODE, 1, 256, 2, 2, 4>(t, blocks, s);
     if (tile == 128) return blocks <= 256 ? launch_product<MODE, 1, 128, 4, 2, 2>(t, blocks, s) : launch_product<MODE, 1, 128, 2, 2, 2>(t, blocks, s);
