@@ -36,31 +36,33 @@ __device__ __forceinline__ float to_float(bf16_t v) { return __uint_as_float(((u
 __device__ __forceinline__ void store(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store(bf16_t* p, float v) { p->bits = bf16_round(v); }
 
-// elements of a 16-byte chunk
-template <typename T> struct Chunk;
-template <> struct Chunk<bf16_t> {
-  static constexpr int kN = 8;
-  static __device__ __forceinline__ void unpack(const u32x4& w, float (&f)[8]) {
-#pragma unroll
-    for (int d = 0; d < 4; ++d) { f[2 * d] = __uint_as_float(w[d] << 16); f[2 * d + 1] = __uint_as_float(w[d] & 0xFFFF0000u); }
+// A chunk of V elements, 4 to 16 bytes, as it lies in memory.
+template <typename T, int V>
+struct Chunk {
+  static constexpr int kWords = V * (int)sizeof(T) / 4;
+  typedef uint32_t Raw __attribute__((ext_vector_type(kWords < 2 ? 2 : kWords)));   // (of one word: the first of two)
+  static __device__ __forceinline__ Raw load(const T* p) {
+    if constexpr (kWords == 1) return Raw{*reinterpret_cast<const uint32_t*>(p), 0u};
+    else return *reinterpret_cast<const Raw*>(p);
   }
-  static __device__ __forceinline__ u32x4 pack(const float (&f)[8]) {
-    u32x4 o;
-#pragma unroll
-    for (int d = 0; d < 4; ++d) o[d] = bf16_pack2(f[2 * d], f[2 * d + 1]);
-    return o;
+  static __device__ __forceinline__ void store(T* p, const Raw& w) {
+    if constexpr (kWords == 1) *reinterpret_cast<uint32_t*>(p) = w[0];
+    else *reinterpret_cast<Raw*>(p) = w;
   }
-};
-template <> struct Chunk<float> {
-  static constexpr int kN = 4;
-  static __device__ __forceinline__ void unpack(const u32x4& w, float (&f)[4]) {
+  static __device__ __forceinline__ void unpack(const Raw& w, float (&f)[V]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(w[e]);
+    for (int d = 0; d < kWords; ++d) {
+      if constexpr (sizeof(T) == 2) { f[2 * d] = __uint_as_float(w[d] << 16); f[2 * d + 1] = __uint_as_float(w[d] & 0xFFFF0000u); }
+      else f[d] = __uint_as_float(w[d]);
+    }
   }
-  static __device__ __forceinline__ u32x4 pack(const float (&f)[4]) {
-    u32x4 o;
+  static __device__ __forceinline__ Raw pack(const float (&f)[V]) {
+    Raw o = {};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(f[e]);
+    for (int d = 0; d < kWords; ++d) {
+      if constexpr (sizeof(T) == 2) o[d] = bf16_pack2(f[2 * d], f[2 * d + 1]);
+      else o[d] = __float_as_uint(f[d]);
+    }
     return o;
   }
 };
@@ -173,28 +175,26 @@ __device__ __forceinline__ void place_of(int r, int heads, float inv_heads, int&
   head = r - token * heads;
 }
 
-// The two 16-byte chunks of a row that a lane holds, as they lie in memory.
-struct Pair { u32x4 c[2]; };
-template <typename T>
-__device__ __forceinline__ Pair load_pair(const T* row, int c0, int c1, bool has0, bool has1) {
-  constexpr int V = Chunk<T>::kN;
-  Pair p = {};
-  if (has0) p.c[0] = *reinterpret_cast<const u32x4*>(row + c0 * V);
-  if (has1) p.c[1] = *reinterpret_cast<const u32x4*>(row + c1 * V);
+// The two chunks of a row that a lane holds.
+template <typename T, int V> struct Pair { typename Chunk<T, V>::Raw c[2]; };
+template <typename T, int V>
+__device__ __forceinline__ Pair<T, V> load_pair(const T* row, int c0, int c1, bool has0, bool has1) {
+  Pair<T, V> p = {};
+  if (has0) p.c[0] = Chunk<T, V>::load(row + c0 * V);
+  if (has1) p.c[1] = Chunk<T, V>::load(row + c1 * V);
   return p;
 }
-template <typename T>
-__device__ __forceinline__ void store_pair(T* row, const Pair& p, int c0, int c1, bool has0, bool has1) {
-  constexpr int V = Chunk<T>::kN;
-  if (has0) *reinterpret_cast<u32x4*>(row + c0 * V) = p.c[0];
-  if (has1) *reinterpret_cast<u32x4*>(row + c1 * V) = p.c[1];
+template <typename T, int V>
+__device__ __forceinline__ void store_pair(T* row, const Pair<T, V>& p, int c0, int c1, bool has0, bool has1) {
+  if (has0) Chunk<T, V>::store(row + c0 * V, p.c[0]);
+  if (has1) Chunk<T, V>::store(row + c1 * V, p.c[1]);
 }
 
-// Rows of whole 16-byte chunks: G lanes a row, two chunks a lane.  Also the backward pass without norm (a rotation by -t).  With norm, queries and
+// Rows of whole chunks of V elements: G lanes a row, two chunks a lane.  Also the backward pass without norm (a rotation by -t).  With norm, queries and
 // keys one after the other, so that a lane holds the weights of its elements; the next row is requested before this one is worked on.
-template <typename T, int G>
+template <typename T, int V, int G>
 __global__ __launch_bounds__(kThreads) void heads_forward_kernel(Args a) {
-  constexpr int V = Chunk<T>::kN, S = kThreads / G;
+  constexpr int S = kThreads / G;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   Token* tok = reinterpret_cast<Token*>(lds);
   float2* cs = reinterpret_cast<float2*>(lds + sizeof(Token) * kMaxTokensPerBlock);
@@ -215,40 +215,40 @@ __global__ __launch_bounds__(kThreads) void heads_forward_kernel(Args a) {
     auto request = [&](int r) {
       int k, h;
       place_of(min(r, rows - 1), heads, inv_heads, k, h);
-      return load_pair(static_cast<const T*>(a.x) + tok[k].x + (h0 + h) * a.xs[2], c0, c1, has0, has1);
+      return load_pair<T, V>(static_cast<const T*>(a.x) + tok[k].x + (h0 + h) * a.xs[2], c0, c1, has0, has1);
     };
-    Pair next = request(threadIdx.x / G), gam = {}, bet = {};
+    Pair<T, V> next = request(threadIdx.x / G), gam = {}, bet = {};
     if (a.norm) {
-      gam = load_pair(static_cast<const T*>(a.gamma) + g * a.dim, c0, c1, has0, has1);
-      if (a.beta) bet = load_pair(static_cast<const T*>(a.beta) + g * a.dim, c0, c1, has0, has1);
+      gam = load_pair<T, V>(static_cast<const T*>(a.gamma) + g * a.dim, c0, c1, has0, has1);
+      if (a.beta) bet = load_pair<T, V>(static_cast<const T*>(a.beta) + g * a.dim, c0, c1, has0, has1);
     }
     for (int r = threadIdx.x / G; r < rows; r += S) {
       int k, h;
       place_of(r, heads, inv_heads, k, h);
       h += h0;
-      const Pair now = next;
+      const Pair<T, V> now = next;
       next = request(r + S);
-      if (a.keep) store_pair(static_cast<T*>(a.keep) + ((size_t)(first + k) * a.heads + h) * a.dim, now, c0, c1, has0, has1);
+      if (a.keep) store_pair<T, V>(static_cast<T*>(a.keep) + ((size_t)(first + k) * a.heads + h) * a.dim, now, c0, c1, has0, has1);
       float u[V], v[V];
-      Chunk<T>::unpack(now.c[0], u);
-      Chunk<T>::unpack(now.c[1], v);
+      Chunk<T, V>::unpack(now.c[0], u);
+      Chunk<T, V>::unpack(now.c[1], v);
       if (a.norm) {
         const float rstd = centre<G>(u, v, has0, has1, inv_dim, a.eps);
         float w[V], z[V];
-        Chunk<T>::unpack(gam.c[0], w);
-        Chunk<T>::unpack(bet.c[0], z);
+        Chunk<T, V>::unpack(gam.c[0], w);
+        Chunk<T, V>::unpack(bet.c[0], z);
 #pragma unroll
         for (int e = 0; e < V; ++e) u[e] = w[e] * (u[e] * rstd) + z[e];
-        Chunk<T>::unpack(gam.c[1], w);
-        Chunk<T>::unpack(bet.c[1], z);
+        Chunk<T, V>::unpack(gam.c[1], w);
+        Chunk<T, V>::unpack(bet.c[1], z);
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] = w[e] * (v[e] * rstd) + z[e];
       }
       if (a.pairs) turn(u, v, cs + k * a.pairs, c0, c1, rotated, a.interleaved);
-      Pair out;
-      out.c[0] = Chunk<T>::pack(u);
-      out.c[1] = Chunk<T>::pack(v);
-      store_pair(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], out, c0, c1, has0, has1);
+      Pair<T, V> out;
+      out.c[0] = Chunk<T, V>::pack(u);
+      out.c[1] = Chunk<T, V>::pack(v);
+      store_pair<T, V>(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], out, c0, c1, has0, has1);
     }
   }
 }
@@ -256,9 +256,9 @@ __global__ __launch_bounds__(kThreads) void heads_forward_kernel(Args a) {
 // Backward pass with norm, queries (blockIdx.y = 0) and keys apart.  Workgroups walk over blocks of tokens and keep the sums for dgamma and dbeta of the
 // elements their lanes hold in registers (one kernel for both kinds of head held twice the sums: two wavefronts a SIMD instead of four, 4096 tokens of
 // 12 + 12 heads of 64 16.4 us); at the end each adds its lanes up through LDS in a fixed order and writes its part of a partial row.
-template <typename T, int G>
+template <typename T, int V, int G>
 __global__ __launch_bounds__(kThreads) void heads_norm_backward_kernel(Args a) {
-  constexpr int V = Chunk<T>::kN, S = kThreads / G;
+  constexpr int S = kThreads / G;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   Token* tok = reinterpret_cast<Token*>(lds);
   float2* cs = reinterpret_cast<float2*>(lds + sizeof(Token) * kMaxTokensPerBlock);
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(kThreads) void heads_norm_backward_kernel(Args a) {
   const float inv_dim = 1.f / (float)a.dim;
   const int g = blockIdx.y, heads = g ? a.heads - a.heads_q : a.heads_q, h0 = g ? a.heads_q : 0, per_block = g ? a.tokens_per_block_k : a.tokens_per_block;
   const float inv_heads = 1.f / (float)heads;
-  const Pair gam = load_pair(static_cast<const T*>(a.gamma) + g * a.dim, c0, c1, has0, has1);
+  const Pair<T, V> gam = load_pair<T, V>(static_cast<const T*>(a.gamma) + g * a.dim, c0, c1, has0, has1);
   float dgam[2][V], dbet[2][V];
 #pragma unroll
   for (int e = 0; e < V; ++e) dgam[0][e] = dgam[1][e] = dbet[0][e] = dbet[1][e] = 0.f;
@@ -279,12 +279,12 @@ __global__ __launch_bounds__(kThreads) void heads_norm_backward_kernel(Args a) {
     __syncthreads();
     load_tokens(a, first, n, tok, cs);
     __syncthreads();
-    struct Both { Pair x, dy; };
+    struct Both { Pair<T, V> x, dy; };
     auto request = [&](int r) {
       int k, h;
       place_of(min(r, rows - 1), heads, inv_heads, k, h);
-      return Both{load_pair(static_cast<const T*>(a.x) + tok[k].x + (h0 + h) * a.xs[2], c0, c1, has0, has1),
-                  load_pair(static_cast<const T*>(a.dy) + tok[k].g + (h0 + h) * a.gs[2], c0, c1, has0, has1)};
+      return Both{load_pair<T, V>(static_cast<const T*>(a.x) + tok[k].x + (h0 + h) * a.xs[2], c0, c1, has0, has1),
+                  load_pair<T, V>(static_cast<const T*>(a.dy) + tok[k].g + (h0 + h) * a.gs[2], c0, c1, has0, has1)};
     };
     Both next = request(threadIdx.x / G);
     for (int r = threadIdx.x / G; r < rows; r += S) {
@@ -294,14 +294,14 @@ __global__ __launch_bounds__(kThreads) void heads_norm_backward_kernel(Args a) {
       const Both now = next;
       next = request(r + S);
       float u[V], v[V], p[V], q[V], w[V];
-      Chunk<T>::unpack(now.x.c[0], u);
-      Chunk<T>::unpack(now.x.c[1], v);
-      Chunk<T>::unpack(now.dy.c[0], p);
-      Chunk<T>::unpack(now.dy.c[1], q);
+      Chunk<T, V>::unpack(now.x.c[0], u);
+      Chunk<T, V>::unpack(now.x.c[1], v);
+      Chunk<T, V>::unpack(now.dy.c[0], p);
+      Chunk<T, V>::unpack(now.dy.c[1], q);
       const float rstd = centre<G>(u, v, has0, has1, inv_dim, a.eps);
       if (a.pairs) turn(p, q, cs + k * a.pairs, c0, c1, rotated, a.interleaved);
       float s1 = 0.f, s2 = 0.f;
-      Chunk<T>::unpack(gam.c[0], w);
+      Chunk<T, V>::unpack(gam.c[0], w);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         u[e] *= rstd;
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(kThreads) void heads_norm_backward_kernel(Args a) {
         s1 += p[e];
         s2 += p[e] * u[e];
       }
-      Chunk<T>::unpack(gam.c[1], w);
+      Chunk<T, V>::unpack(gam.c[1], w);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         v[e] *= rstd;
@@ -324,10 +324,10 @@ __global__ __launch_bounds__(kThreads) void heads_norm_backward_kernel(Args a) {
       const float m1 = group_sum<G>(s1) * inv_dim, m2 = group_sum<G>(s2) * inv_dim;
 #pragma unroll
       for (int e = 0; e < V; ++e) { u[e] = (p[e] - m1 - u[e] * m2) * rstd; v[e] = (q[e] - m1 - v[e] * m2) * rstd; }
-      Pair out;
-      out.c[0] = Chunk<T>::pack(u);
-      out.c[1] = Chunk<T>::pack(v);
-      store_pair(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], out, c0, c1, has0, has1);
+      Pair<T, V> out;
+      out.c[0] = Chunk<T, V>::pack(u);
+      out.c[1] = Chunk<T, V>::pack(v);
+      store_pair<T, V>(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], out, c0, c1, has0, has1);
     }
   }
   // [lane groups][2][dim] floats.  A column's lane groups are added up by as many threads as there are columns for, each a stretch of
@@ -523,7 +523,7 @@ __global__ __launch_bounds__(kThreads) void heads_norm_backward_any_kernel(Args 
 }
 
 struct Route {
-  int lanes = 0;             // lanes a row of the kernels of whole chunks, 0: the general kernels
+  int lanes = 0, elements = 0;   // lanes a row and elements a chunk of the kernels of whole chunks, 0: the general kernels
   int tokens_per_block = 1, tokens_per_block_k = 1;
   long long blocks = 0;
   int kinds = 1;             // blockIdx.y: queries, keys (backward with norm)
@@ -540,13 +540,16 @@ constexpr long long kBackwardBlocks = 512;
 Route route_of(const HeadsProblem& q, bool sums) {
   Route r;
   const long long tokens = (long long)q.batch * q.seq;
-  const int v = q.dtype == DType::BF16 ? 8 : 4;
-  auto whole = [&](const long long (&s)[3]) { return s[0] % v == 0 && s[1] % v == 0 && s[2] % v == 0; };
-  const bool strides = whole(q.x_stride) && whole(q.out_stride) && (!q.dy || whole(q.dy_stride));
+  // the widest chunks of 16, 8 or 4 bytes that divide the head, the pairs and every stride, from aligned addresses
+  const int size = q.dtype == DType::BF16 ? 2 : 4;
   const uintptr_t bits = (uintptr_t)q.x | (uintptr_t)q.dy | (uintptr_t)q.out | (uintptr_t)q.gamma | (uintptr_t)q.beta | (uintptr_t)q.keep;
-  const bool pairs = q.interleaved ? 2 * q.pairs % v == 0 : q.pairs % v == 0;
-  if (q.head_dim % v == 0 && strides && (bits & 15) == 0 && pairs) {
-    r.lanes = 1;
+  for (int v = 16 / size; v >= 2 && !r.lanes; v /= 2) {
+    auto whole = [&](const long long (&s)[3]) { return s[0] % v == 0 && s[1] % v == 0 && s[2] % v == 0; };
+    const bool strides = whole(q.x_stride) && whole(q.out_stride) && (!q.dy || whole(q.dy_stride));
+    const bool pairs = q.interleaved ? 2 * q.pairs % v == 0 : q.pairs % v == 0;
+    if (q.head_dim % v || !strides || bits % (v * size) || !pairs) continue;
+    r.elements = v;
+    r.lanes = v == 16 / size ? 1 : v == 2 ? 8 : 4;   // (few lanes only where all of a head is little: with wide chunks)
     while (r.lanes * 2 * v < q.head_dim) r.lanes *= 2;
   }
   const int at_once = r.lanes ? kThreads / r.lanes : kThreads / 64;   // rows a workgroup works on at a time
@@ -587,34 +590,20 @@ hipError_t launch(F* kernel, const Route& r, const Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T>
-hipError_t launch_forward(const Route& r, const Args& a, hipStream_t s) {
-  switch (r.lanes) {
-    case 0: return launch(heads_forward_any_kernel<T>, r, a, s);
-    case 1: return launch(heads_forward_kernel<T, 1>, r, a, s);
-    case 2: return launch(heads_forward_kernel<T, 2>, r, a, s);
-    case 4: return launch(heads_forward_kernel<T, 4>, r, a, s);
-    case 8: return launch(heads_forward_kernel<T, 8>, r, a, s);
-    case 16: return launch(heads_forward_kernel<T, 16>, r, a, s);
-    case 32:
-      if constexpr (std::is_same_v<T, float>) return launch(heads_forward_kernel<T, 32>, r, a, s);
-      break;
-  }
-  return hipErrorInvalidValue;
+template <typename T, int V, int G>
+hipError_t launch_lanes(bool backward, const Route& r, const Args& a, hipStream_t s) {
+  if (r.lanes == G) return backward ? launch(heads_norm_backward_kernel<T, V, G>, r, a, s) : launch(heads_forward_kernel<T, V, G>, r, a, s);
+  if constexpr (2 * G * V < SPB_MAX_HEAD_DIM) return launch_lanes<T, V, 2 * G>(backward, r, a, s);   // a longer head
+  else return hipErrorInvalidValue;
 }
+// backward: with norm
 template <typename T>
-hipError_t launch_norm_backward(const Route& r, const Args& a, hipStream_t s) {
-  switch (r.lanes) {
-    case 0: return launch(heads_norm_backward_any_kernel<T>, r, a, s);
-    case 1: return launch(heads_norm_backward_kernel<T, 1>, r, a, s);
-    case 2: return launch(heads_norm_backward_kernel<T, 2>, r, a, s);
-    case 4: return launch(heads_norm_backward_kernel<T, 4>, r, a, s);
-    case 8: return launch(heads_norm_backward_kernel<T, 8>, r, a, s);
-    case 16: return launch(heads_norm_backward_kernel<T, 16>, r, a, s);
-    case 32:
-      if constexpr (std::is_same_v<T, float>) return launch(heads_norm_backward_kernel<T, 32>, r, a, s);
-      break;
-  }
+hipError_t launch_heads(bool backward, const Route& r, const Args& a, hipStream_t s) {
+  constexpr int kWide = 16 / (int)sizeof(T);
+  if (r.lanes == 0) return backward ? launch(heads_norm_backward_any_kernel<T>, r, a, s) : launch(heads_forward_any_kernel<T>, r, a, s);
+  if (r.elements == kWide) return launch_lanes<T, kWide, 1>(backward, r, a, s);
+  if (r.elements == 2) return launch_lanes<T, 2, 8>(backward, r, a, s);
+  if constexpr (kWide == 8) return launch_lanes<T, 4, 4>(backward, r, a, s);
   return hipErrorInvalidValue;
 }
 
@@ -629,7 +618,7 @@ hipError_t launch_heads_forward(const HeadsProblem& q, hipStream_t s) {
   if (!valid(q) || !q.x) return hipErrorInvalidValue;
   const Route r = route_of(q, false);
   const Args a = args_of(q, r, false);
-  return q.dtype == DType::BF16 ? launch_forward<bf16_t>(r, a, s) : launch_forward<float>(r, a, s);
+  return q.dtype == DType::BF16 ? launch_heads<bf16_t>(false, r, a, s) : launch_heads<float>(false, r, a, s);
 }
 
 size_t heads_partial_floats(int batch, int seq, int heads_k, int head_dim) {
@@ -645,12 +634,12 @@ hipError_t launch_heads_backward(const HeadsProblem& q, hipStream_t s, ReduceTas
     for (int i = 0; i < 3; ++i) b.x_stride[i] = q.dy_stride[i];
     const Route r = route_of(b, false);
     const Args a = args_of(b, r, true);
-    return q.dtype == DType::BF16 ? launch_forward<bf16_t>(r, a, s) : launch_forward<float>(r, a, s);
+    return q.dtype == DType::BF16 ? launch_heads<bf16_t>(false, r, a, s) : launch_heads<float>(false, r, a, s);
   }
   if (!q.x || !q.partial || !q.dgamma || !q.dbeta) return hipErrorInvalidValue;
   const Route r = route_of(q, true);
   const Args a = args_of(q, r, true);
-  const hipError_t e = q.dtype == DType::BF16 ? launch_norm_backward<bf16_t>(r, a, s) : launch_norm_backward<float>(r, a, s);
+  const hipError_t e = q.dtype == DType::BF16 ? launch_heads<bf16_t>(true, r, a, s) : launch_heads<float>(true, r, a, s);
   if (e != hipSuccess) return e;
   ReduceTask task;
   task.kind = ReduceTask::kPairs;

@@ -125,6 +125,13 @@ CASES = {
     "heads_first": dict(b=3, s=29, hq=4, hk=4, d=64, layout="heads", sections=(32,), shared_pos=True),
     "odd_size": dict(b=2, s=31, hq=3, hk=2, d=100, sections=(25, 25)),
     "odd_size_norm": dict(b=2, s=31, hq=3, hk=2, d=37, sections=(5, 4)),
+    "eight_byte_chunks": dict(b=2, s=33, hq=5, hk=3, d=72, sections=(18, 18)),
+    "eight_byte_chunks_256": dict(b=1, s=23, hq=2, hk=2, d=252, sections=(60, 60)),
+    "four_byte_chunks": dict(b=2, s=33, hq=5, hk=3, d=106, sections=(20, 14, 14), interleaved=True),
+    "four_byte_chunks_small": dict(b=2, s=33, hq=5, hk=0, d=6, sections=(2,)),
+    "four_byte_chunks_254": dict(b=1, s=23, hq=2, hk=2, d=254, sections=(64, 62)),
+    "f32_eight_byte_chunks": dict(b=2, s=21, hq=2, hk=1, d=38, dtype=torch.float32, sections=(10, 8)),
+    "odd_pairs": dict(b=2, s=31, hq=3, hk=2, d=100, sections=(25,)),
     "odd_start": dict(b=2, s=19, hq=4, hk=4, d=64, layout="odd", sections=(16, 16), interleaved=True),
     "whole_255": dict(b=1, s=13, hq=1, hk=1, d=255, sections=(127,)),
     "f32": dict(b=2, s=45, hq=6, hk=6, d=64, dtype=torch.float32, sections=(16, 8, 8), far=10 ** 6),
