@@ -113,7 +113,7 @@ EXPORTS = {
     "spb_worker_depth": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_int32)]),
     "spb_aggregate_update": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                        C.c_float, C.c_float, C.c_float, C.c_int32, C.c_void_p]),
-    "spb_rotary_sections": (C.c_int, [C.POINTER(spb_rotary), C.c_int32, C.POINTER(C.c_int32), C.c_double, C.c_int32, C.c_int32]),
+    "spb_rotary_sections": (C.c_int, [C.POINTER(spb_rotary), C.c_int32, C.c_void_p, C.c_double, C.c_int32, C.c_int32]),
     "spb_heads_forward": (C.c_int, [C.POINTER(spb_heads_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
     "spb_heads_workspace_size": (C.c_int, [C.POINTER(spb_heads_desc), C.POINTER(C.c_size_t)]),
     "spb_heads_backward": (C.c_int, [C.POINTER(spb_heads_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p,
@@ -296,11 +296,14 @@ def spb_aggregate_update(m, depths, worker_grads, velocity, lr, momentum, weight
                                       int(bool(scale_lr)), C.c_void_p(stream)))
 
 
+_NO_SECTIONS = array.array("i", [0])
+
+
 def spb_rotary_sections(sections, base=10000.0, own_ladder=False, interleaved=False) -> spb_rotary:
     """Rotary description: sections[a] pairs for axis a; see spb.h for the frequencies."""
     out = spb_rotary()
-    _check(lib().spb_rotary_sections(C.byref(out), len(sections), (C.c_int32 * max(1, len(sections)))(*sections), base, int(bool(own_ladder)),
-                                     int(bool(interleaved))))
+    counts = array.array("i", sections) or _NO_SECTIONS
+    _check(lib().spb_rotary_sections(out, len(sections), counts.buffer_info()[0], base, 1 if own_ladder else 0, 1 if interleaved else 0))
     return out
 
 
@@ -327,23 +330,28 @@ _HEADS = struct.Struct("<7if9q")       # spb_heads_desc up to its rotary
 assert _HEADS.size == spb_heads_desc.rotary.offset
 
 
+def _like(t, x, shape, name):
+    if t.shape != shape or t.dtype is not x.dtype:
+        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, x is {tuple(shape)} of {x.dtype}")
+    return t.stride()
+
+
 def heads_desc(x, heads_q, y=None, dx=None, norm=False, eps=1e-5, rotary=None) -> spb_heads_desc:
     """Description of a spb_heads_forward call on x and y, or a spb_heads_backward call on x, dy (passed as y) and dx: tensors
     [batch, seq, heads, head_dim] of one dtype and any strides but that of the head's elements.  The first heads_q heads are queries, the
     rest keys.  y and dx default to x's strides."""
     d = spb_heads_desc()
-    shape, dtype, sx = x.shape, x.dtype, x.stride()
+    shape, sx = x.shape, x.stride()
     batch, seq, heads, dim = shape
-    strides = [sx, sx, sx]
-    for i, t in ((1, y), (2, dx)):
-        if t is not None:
-            if t.shape != shape or t.dtype != dtype:
-                raise ValueError(f"{'x y dx'.split()[i]}: {tuple(t.shape)} of {t.dtype}, x is {tuple(shape)} of {dtype}")
-            strides[i] = t.stride()
-    sy, sd = strides[1:]
+    sy = sd = sx
+    if y is not None:
+        sy = _like(y, x, shape, "y")
+    if dx is not None:
+        sd = _like(dx, x, shape, "dx")
     if dim > 1 and not sx[3] == sy[3] == sd[3] == 1:
         raise ValueError("the elements of a head must be contiguous")
-    _HEADS.pack_into(d, 0, _dtype_code(x), batch, seq, heads_q, heads - heads_q, dim, 1 if norm else 0, eps, *sx[:3], *sy[:3], *sd[:3])
+    _HEADS.pack_into(d, 0, _dtype_code(x), batch, seq, heads_q, heads - heads_q, dim, 1 if norm else 0, eps, sx[0], sx[1], sx[2], sy[0], sy[1], sy[2],
+                     sd[0], sd[1], sd[2])
     if rotary is not None:
         d.rotary = rotary
     return d
@@ -354,11 +362,12 @@ def _positions(desc, pos):
     if pos is None:
         return None, 0, 0
     import torch
-    if pos.dtype != torch.int32 or pos.dim() != 3:
-        raise ValueError(f"positions are int32 [axes, batch, seq], not {pos.dtype} {tuple(pos.shape)}")
-    (axes, batch, seq), (by_axis, by_batch, by_token) = pos.shape, pos.stride()
-    if axes < desc.rotary.axes or batch not in (1, desc.batch) or seq != desc.seq or (seq > 1 and by_token != 1):
-        raise ValueError(f"positions {tuple(pos.shape)} (last stride {by_token}) for {desc.rotary.axes} axes of {desc.batch} x {desc.seq} tokens")
+    shape = pos.shape
+    if pos.dtype is not torch.int32 or len(shape) != 3:
+        raise ValueError(f"positions are int32 [axes, batch, seq], not {pos.dtype} {tuple(shape)}")
+    (axes, batch, seq), (by_axis, by_batch, by_token) = shape, pos.stride()
+    if axes < desc.rotary.axes or (batch != 1 and batch != desc.batch) or seq != desc.seq or (by_token != 1 and seq > 1):
+        raise ValueError(f"positions {tuple(shape)} (last stride {by_token}) for {desc.rotary.axes} axes of {desc.batch} x {desc.seq} tokens")
     return pos.data_ptr(), by_axis, 0 if batch == 1 else by_batch
 
 
@@ -417,39 +426,42 @@ _MUON = struct.Struct("<4Q2qd4i")      # spb_muon_tensor
 assert _MUON.size == C.sizeof(spb_muon_tensor)
 
 
-def _muon_tensors(tensors):
+def _muon_tensors(tensors, pointers=True):
     """ctypes list of tensors given as dict(w, m, v=None, grads=[...], blocks=0, rate_scale=1.0), and what keeps its arrays alive.  A
-    stack [blocks, rows, cols] is its matrices' rows one after the other; any other tensor has its first dimension as rows."""
-    import torch
-    f32 = torch.float32
+    stack [blocks, rows, cols] is its matrices' rows one after the other; any other tensor has its first dimension as rows.  Without
+    pointers: shapes only."""
+    from torch import float32
     arr = (spb_muon_tensor * max(1, len(tensors)))()
-    pointers = array.array("Q", [g.data_ptr() for t in tensors for g in t["grads"]])
-    at = pointers.buffer_info()[0]
+    held = array.array("Q", [g.data_ptr() for t in tensors for g in t["grads"]] if pointers else ())
+    at = held.buffer_info()[0]
     for i, t in enumerate(tensors):
-        w, m, v, grads, blocks = t["w"], t["m"], t.get("v"), t["grads"], t.get("blocks", 0)
-        shape = w.shape
-        good = w.is_contiguous()
-        for x in (m, *grads) if v is None else (m, v, *grads):
-            good = good and x.dtype == f32 and x.shape == shape and x.is_contiguous()
-        if not good:
-            raise ValueError("m, v and gradients are contiguous float32 tensors of the parameter's shape, which is contiguous too")
-        stack = blocks >= 1 and len(shape) == 3 and shape[0] == blocks
-        rows = shape[0] * shape[1] if stack else (shape[0] if shape else 1)
-        _MUON.pack_into(arr, i * _MUON.size, w.data_ptr(), m.data_ptr(), 0 if v is None else v.data_ptr(), at, rows, w.numel() // rows if rows else 0,
-                        t.get("rate_scale", 1.0), len(grads), _dtype_code(w), blocks, 0)
-        at += 8 * len(grads)
-    return arr, pointers
+        w, blocks = t["w"], t.get("blocks", 0)
+        shape, where, count = w.shape, (0, 0, 0, 0), 0
+        if pointers:
+            m, v, grads = t["m"], t.get("v"), t["grads"]
+            good = w.is_contiguous()
+            for x in (m, *grads) if v is None else (m, v, *grads):
+                good = good and x.dtype is float32 and x.shape == shape and x.is_contiguous()
+            if not good:
+                raise ValueError("m, v and gradients are contiguous float32 tensors of the parameter's shape, which is contiguous too")
+            where, count = (w.data_ptr(), m.data_ptr(), 0 if v is None else v.data_ptr(), at), len(grads)
+            at += 8 * count
+        dims = len(shape)
+        rows = shape[0] * shape[1] if dims == 3 and blocks >= 1 and shape[0] == blocks else shape[0] if dims else 1
+        _MUON.pack_into(arr, i * _MUON.size, *where, rows, w.numel() // rows if rows else 0, t.get("rate_scale", 1.0), count, _dtype_code(w), blocks, 0)
+    return arr, held
 
 
 def spb_muon_workspace_size(tensors) -> int:
-    arr, _keep = _muon_tensors(tensors)
+    """Shapes, types and blocks of the tensors are all it looks at."""
+    arr, _ = _muon_tensors(tensors, pointers=False)
     n = C.c_size_t()
-    _check(lib().spb_muon_workspace_size(arr, len(tensors), C.byref(n)))
+    _check(lib().spb_muon_workspace_size(arr, len(tensors), n))
     return n.value
 
 
 def spb_muon_step(tensors, config: spb_muon_config, workspace, workspace_bytes, stream):
-    arr, _keep = _muon_tensors(tensors)
+    arr, _held = _muon_tensors(tensors)
     _check(lib().spb_muon_step(arr, len(tensors), config, _address(workspace), workspace_bytes, stream))
 
 

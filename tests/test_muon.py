@@ -348,10 +348,9 @@ def test_workspace_sizes():
     assert spb.spb_muon_workspace_size([_tensor((50,), 0, torch.float32, 1, 0, device="cpu")]) == 0 == spb.spb_muon_workspace_size([])
     wide = _tensor((96, 216), 1, torch.float32, 1, 0, device="cpu")
     assert spb.spb_muon_workspace_size([wide]) > spb.spb_muon_workspace_size([flat])
-    with pytest.raises(ValueError):
-        spb.spb_muon_workspace_size([dict(flat, m=flat["m"].T)])
-    with pytest.raises(ValueError):
-        spb.spb_muon_workspace_size([dict(flat, grads=[flat["grads"][0].double()])])
+    for bad in (dict(m=flat["m"].T), dict(m=flat["m"].reshape(216, 96)), dict(grads=[flat["grads"][0].double()]), dict(w=flat["w"].T)):
+        with pytest.raises(ValueError):
+            spb.spb_muon_step([{**flat, **bad}], spb.muon_config(**HYPER), None, 0, 0)
 
 
 def test_server_step_arguments():
