@@ -45,7 +45,7 @@ struct Matrix {
   void* w;                 // first element of the matrix in its parameter
   const float* u;          // [rows, cols] dense
   const double* partial;   // [parts] sums of u^2
-  int parts, rows, cols, vector;   // vector: 8 entries of a row are whole 16-byte pieces
+  int parts, rows, cols, bf16, vector;   // vector: 8 entries of a row are whole 16-byte pieces
   float keep, step, eps;   // w = keep * w - step * X
 };
 
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(kThreads) void update_kernel(Table tab) {
     t.partial[(long long)mat * t.parts + part] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     if (part == 0)
       t.out[mat] = Matrix{t.bf16 ? (void*)(static_cast<uint16_t*>(t.w) + base) : (void*)(static_cast<float*>(t.w) + base), t.u + base,
-                          t.partial + (long long)mat * t.parts, t.parts, t.rows, t.cols, t.vector && t.cols % 8 == 0, t.keep, t.step, tab.ns_eps};
+                          t.partial + (long long)mat * t.parts, t.parts, t.rows, t.cols, t.bf16, t.vector && t.cols % 8 == 0, t.keep, t.step, tab.ns_eps};
   }
 }
 
@@ -211,15 +211,28 @@ struct Groups {
   int n;
 };
 
-__device__ __forceinline__ const Group& group_of(const Groups& t, int block, int& mat, int& tile) {
-  int i = 0;
-  for (int j = 1; j < t.n; ++j)
-    if (block >= t.g[j].first_block) i = j;
-  const Group& g = t.g[i];
-  const int local = block - g.first_block;
-  mat = local / g.per_matrix;
-  tile = local - mat * g.per_matrix;
-  return g;
+// EARLY: by value, the first group at once, which saves small launches a second round trip to the kernel's arguments (66 -> 58 us for a step of one
+// 100 x 300 matrix); the large kernels lose 5 % to holding it.
+template <bool EARLY>
+__device__ __forceinline__ std::conditional_t<EARLY, Group, const Group&> group_of(const Groups& t, int block, int& mat, int& tile) {
+  if constexpr (EARLY) {
+    Group g = t.g[0];
+    for (int j = 1; j < t.n; ++j)
+      if (block >= t.g[j].first_block) g = t.g[j];
+    const int local = block - g.first_block;
+    mat = local / g.per_matrix;
+    tile = local - mat * g.per_matrix;
+    return g;
+  } else {
+    int i = 0;
+    for (int j = 1; j < t.n; ++j)
+      if (block >= t.g[j].first_block) i = j;
+    const Group& g = t.g[i];
+    const int local = block - g.first_block;
+    mat = local / g.per_matrix;
+    tile = local - mat * g.per_matrix;
+    return g;
+  }
 }
 
 // value and remainder of v at p and, with two planes, p + plane
@@ -254,7 +267,7 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(Groups groups) {
   __shared__ float tile_s[64][65];
   __shared__ double sums[kThreads / 64];
   int mat, tile;
-  const Group& g = group_of(groups, blockIdx.x, mat, tile);
+  const Group g = group_of<true>(groups, blockIdx.x, mat, tile);
   const Matrix d = g.matrices[mat];
   double s = (int)threadIdx.x < d.parts ? d.partial[threadIdx.x] : 0.0;
 #pragma unroll
@@ -429,7 +442,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(Groups 
   static_assert((size_t)NW * 32 * (WN + 4) * 4 <= (size_t)STAGES * kStageBytes, "epilogue staging fits in the ring");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   int mat, tile;
-  const Group& g = group_of(groups, xcd_tile(blockIdx.x, gridDim.x), mat, tile);
+  const Group& g = group_of<false>(groups, xcd_tile(blockIdx.x, gridDim.x), mat, tile);
   int ti, tj;
   place_tile<MODE>(tile, g.mp / BT, ti, tj);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -653,7 +666,7 @@ __global__ __launch_bounds__(kThreads) void small_product_kernel(Groups groups) 
   constexpr Layout LQ = MODE == kGram || MODE == kPoly ? Layout::RowK : Layout::KRow;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   int mat, tile, ti, tj;
-  const Group& g = group_of(groups, xcd_tile(blockIdx.x, gridDim.x), mat, tile);
+  const Group g = group_of<true>(groups, xcd_tile(blockIdx.x, gridDim.x), mat, tile);
   place_tile<MODE>(tile, g.mp / BT, ti, tj);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const size_t plane_x = (size_t)g.mp * g.np, plane_a = (size_t)g.mp * g.mp;
@@ -774,6 +787,272 @@ __global__ __launch_bounds__(kThreads) void small_product_kernel(Groups groups) 
   }
 }
 
+// ---- matrices with a short side of at most 48 -----------------------------------------------------------------------
+
+// The steps' polynomials commute with A = X X^T, so for a matrix of a short side the whole chain can run on that one small matrix: with
+// B_k = a I + b A_k + c A_k^2,  A_{k+1} = A_k B_k^2  and  X_steps = (B_{steps-1} ... B_0) X_0.  That squares singular values, and rounding in A_0 grows
+// up to a^2 = 11.9 times a step where they are small: in float32 too much of it, in float64 at most 1e-16 * 11.9^7 = 3e-9 by the eighth step, which
+// is where it is used.  Three launches in place of three a step: the entries of A in float64 from slices of the long side, one workgroup a matrix
+// for the chain, the product with u and the update.  16 x 100: 26 us a step of the optimiser, 32 x 300 33, 48 x 300 47, where the products of the whole matrix
+// take 58, most of it 17 launches; a short side of 64 took 66 to 86 us this way (the chain 50, bound by one CU's float64 matrix rate and LDS).
+constexpr int kNarrow = 48, kNarrowLong = 8192, kNarrowSteps = 8, kNarrowCount = 256, kMaxSlices = 16, kNarrowTiles = 6;
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+
+struct NarrowGroup {
+  const Matrix* matrices;
+  double* partial;         // [count][slices][tiles][256]: 16 x 16 tiles of u u^T on and below the diagonal
+  float* q;                // [count][shorter][shorter], and behind the matrices [count] factors 1 / (|u| + eps)
+  int shorter, longer, count, tiles, slices, first_block;
+};
+struct NarrowGroups {
+  NarrowGroup g[kMaxGroups];
+  int n;
+};
+// which matrix of which group, and which of its `per` workgroups
+template <class F>
+__device__ __forceinline__ NarrowGroup narrow_group(const NarrowGroups& t, int block, F&& per, int& mat, int& part) {
+  NarrowGroup g = t.g[0];
+  for (int j = 1; j < t.n; ++j)
+    if (block >= t.g[j].first_block) g = t.g[j];
+  const int local = block - g.first_block, p = per(g);
+  mat = local / p;
+  part = local - mat * p;
+  return g;
+}
+// Row and column of tile number t on and below the diagonal (at most six).
+__device__ __forceinline__ void lower_tile(int t, int& ti, int& tj) {
+  ti = t >= 3 ? 2 : t >= 1 ? 1 : 0;
+  tj = t - ti * (ti + 1) / 2;
+}
+// u's entries of P positions of the long side from `at` on, P / 4 of them a thread; which row of the short side and which position entry k of the thread is.
+template <int P>
+struct NarrowChunk {
+  static constexpr int kEach = P / 4;
+  int shorter, longer;
+  float inv;               // 1 / shorter: entries are numbered below 2^12, which float32 divides exactly
+  bool tall;
+  __device__ __forceinline__ bool place(int k, int& i, int& j) const {
+    const int e = k * kThreads + threadIdx.x;
+    if (tall) { j = (int)(((float)e + 0.5f) * inv); i = e - j * shorter; }
+    else { i = e / P; j = e % P; }
+    return i < shorter && j < P;
+  }
+  __device__ __forceinline__ void load(const float* u, int at, float (&v)[kEach]) const {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      int i, j;
+      const bool has = place(k, i, j) && at + j < longer;
+      v[k] = has ? u[tall ? (size_t)(at + j) * shorter + i : (size_t)i * longer + at + j] : 0.f;
+    }
+  }
+  // to[i][j] = by * v
+  template <int LD>
+  __device__ __forceinline__ void park(const float (&v)[kEach], float by, float (*to)[LD]) const {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      int i, j;
+      if (place(k, i, j)) to[i][j] = v[k] * by;
+    }
+  }
+};
+
+__global__ __launch_bounds__(kThreads) void narrow_gram_kernel(NarrowGroups groups) {
+  __shared__ float xs[kNarrow][65];
+  __shared__ double sums[4 * kNarrowTiles * 256];   // [4 wavefronts][tiles][256]
+  int mat, slice;
+  const NarrowGroup g = narrow_group(groups, blockIdx.x, [](const NarrowGroup& q) { return q.slices; }, mat, slice);
+  const Matrix d = g.matrices[mat];
+  const NarrowChunk<64> chunk = {g.shorter, g.longer, 1.f / (float)g.shorter, d.rows > d.cols};
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m16 = (g.shorter + 15) / 16;
+  for (int e = threadIdx.x; e < kNarrow * 65; e += kThreads) (&xs[0][0])[e] = 0.f;   // rows beyond the short side stay so
+  f64x4 acc[kNarrowTiles];
+#pragma unroll
+  for (int t = 0; t < kNarrowTiles; ++t) acc[t] = f64x4{0.0, 0.0, 0.0, 0.0};
+  float next[16];
+  const int step = 64 * g.slices;
+  chunk.load(d.u, slice * 64, next);
+  for (int at = slice * 64; at < g.longer; at += step) {
+    __syncthreads();
+    chunk.park(next, 1.f, xs);
+    __syncthreads();
+    chunk.load(d.u, at + step, next);
+    // a wavefront takes a quarter of the positions, for all tiles
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int j = wave * 16 + s * 4 + (lane >> 4);
+      double row[kNarrow / 16];
+#pragma unroll
+      for (int t = 0; t < kNarrow / 16; ++t) row[t] = t < m16 ? (double)xs[t * 16 + (lane & 15)][j] : 0.0;
+#pragma unroll
+      for (int t = 0; t < kNarrowTiles; ++t) {
+        int ti, tj;
+        lower_tile(t, ti, tj);
+        if (ti < m16) acc[t] = __builtin_amdgcn_mfma_f64_16x16x4f64(row[ti], row[tj], acc[t], 0, 0, 0);   // uniform
+      }
+    }
+  }
+  double* mine = sums + wave * (kNarrowTiles * 256);
+#pragma unroll
+  for (int t = 0; t < kNarrowTiles; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) mine[t * 256 + (4 * r + (lane >> 4)) * 16 + (lane & 15)] = acc[t][r];
+  __syncthreads();
+  double* out = g.partial + ((size_t)mat * g.slices + slice) * g.tiles * 256;
+  for (int e = threadIdx.x; e < g.tiles * 256; e += kThreads)
+    out[e] = (sums[e] + sums[kNarrowTiles * 256 + e]) + (sums[2 * kNarrowTiles * 256 + e] + sums[3 * kNarrowTiles * 256 + e]);
+}
+
+// doubles from row to row in LDS: 16 rows of 4 consecutive entries, as an operand is read, lie in as many places
+constexpr int narrow_pitch(int m16) { return 16 * m16 + 4; }
+constexpr size_t narrow_lds(int m16) { return (4 * 16 * (size_t)m16 * narrow_pitch(m16) + 2) * sizeof(double); }
+
+// A wavefront a tile on and below the diagonal: the matrix cores of a CU take them in turn.
+constexpr int kChainThreads = 64 * kNarrowTiles;
+template <int M16>
+__device__ __forceinline__ void narrow_chain(const NarrowGroup& g, int mat, int steps, double* a) {
+  constexpr int kPitch = narrow_pitch(M16), kSize = 16 * M16 * kPitch, kTiles = M16 * (M16 + 1) / 2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  double* b = a + kSize;
+  double* t = b + kSize;
+  double* q = t + kSize;
+  double* norm = q + kSize;
+  auto put = [&](double* m, int i, int j, double v) { m[i * kPitch + j] = v; m[j * kPitch + i] = v; };
+  for (int e = threadIdx.x; e < kTiles * 256; e += kChainThreads) {
+    int ti, tj;
+    lower_tile(e >> 8, ti, tj);
+    const double* p = g.partial + (size_t)mat * g.slices * kTiles * 256 + e;
+    double s = 0.0;
+#pragma unroll 8
+    for (int i = 0; i < g.slices; ++i) s += p[(size_t)i * kTiles * 256];
+    const int i = ti * 16 + ((e >> 4) & 15), j = tj * 16 + (e & 15);
+    if (i >= j) put(a, i, j, s);
+  }
+  __syncthreads();
+  if (wave == 0) {   // the trace is |u|^2
+    double s = lane < 16 * M16 ? a[lane * kPitch + lane] : 0.0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (lane == 0) *norm = 1.0 / (sqrt(s) + (double)g.matrices[mat].eps);
+  }
+  __syncthreads();
+  const double inv = *norm;
+  for (int e = threadIdx.x; e < kSize; e += kChainThreads) a[e] = a[e] * inv * inv;
+  __syncthreads();
+  int ti, tj;
+  lower_tile(wave, ti, tj);
+  // out = finish(p r) for symmetric p and r whose product is symmetric: tiles on and below the diagonal, each written twice
+  auto product = [&](const double* p, const double* r, double* out, auto finish) {
+    if (wave < kTiles) {
+      const double* pi = p + (ti * 16 + (lane & 15)) * kPitch + (lane >> 4);
+      const double* rj = r + (tj * 16 + (lane & 15)) * kPitch + (lane >> 4);
+      double x[4 * M16], y[4 * M16];
+#pragma unroll
+      for (int s = 0; s < 4 * M16; ++s) { x[s] = pi[4 * s]; y[s] = rj[4 * s]; }
+      f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+      for (int s = 0; s < 4 * M16; ++s) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(x[s], y[s], acc, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = ti * 16 + 4 * e + (lane >> 4), j = tj * 16 + (lane & 15);
+        if (i >= j) put(out, i, j, finish(acc[e], i, j));
+      }
+    }
+    __syncthreads();
+  };
+  auto as_is = [](double v, int, int) { return v; };
+  for (int k = 0; k < steps; ++k) {
+    product(a, a, b, [&](double v, int i, int j) { return (double)kC * v + (double)kB * a[i * kPitch + j] + (i == j ? (double)kA : 0.0); });
+    if (k > 0) {
+      product(q, b, t, as_is);
+      double* old = q;
+      q = t; t = old;
+    }
+    if (k + 1 == steps) break;
+    product(a, b, t, as_is);
+    product(t, b, a, as_is);
+    if (k == 0) {            // the chain's product so far is B itself
+      double* spare = q;
+      q = b; b = spare;
+    }
+  }
+  const double* chain = steps == 1 ? b : q;
+  float* out = g.q + (size_t)mat * g.shorter * g.shorter;
+  for (int e = threadIdx.x; e < g.shorter * g.shorter; e += kChainThreads) out[e] = (float)chain[(e / g.shorter) * kPitch + e % g.shorter];
+  if (threadIdx.x == 0) g.q[(size_t)g.count * g.shorter * g.shorter + mat] = (float)inv;
+}
+
+__global__ __launch_bounds__(kChainThreads) void narrow_chain_kernel(NarrowGroups groups, int steps) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  int mat, none;
+  const NarrowGroup g = narrow_group(groups, blockIdx.x, [](const NarrowGroup&) { return 1; }, mat, none);
+  double* a = reinterpret_cast<double*>(lds);
+  switch (g.tiles) {   // uniform over the workgroup
+    case 1: narrow_chain<1>(g, mat, steps, a); break;
+    case 3: narrow_chain<2>(g, mat, steps, a); break;
+    default: narrow_chain<3>(g, mat, steps, a);
+  }
+}
+
+// w = keep * w - step * Q u / (|u| + eps), 32 positions of the long side a workgroup, 4 x 2 entries a thread.
+constexpr int kApply = 32;
+__global__ __launch_bounds__(kThreads) void narrow_apply_kernel(NarrowGroups groups) {
+  __shared__ __attribute__((aligned(16))) float us[kNarrow][kApply + 4], qs[kNarrow][64 + 4];   // [k][j], [k][i]
+  int mat, part;
+  const NarrowGroup g = narrow_group(groups, blockIdx.x, [](const NarrowGroup& q) { return (q.longer + kApply - 1) / kApply; }, mat, part);
+  const Matrix d = g.matrices[mat];
+  const float* q = g.q + (size_t)mat * g.shorter * g.shorter;
+  const float inv = g.q[(size_t)g.count * g.shorter * g.shorter + mat];
+  constexpr int kRows = kNarrow / 4;
+  float qv[kRows];
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const int row = k * 4 + (threadIdx.x >> 6), i = threadIdx.x & 63;
+    qv[k] = row < g.shorter && i < g.shorter ? q[row * g.shorter + i] : 0.f;   // (symmetric)
+  }
+  const bool tall = d.rows > d.cols;
+  const NarrowChunk<kApply> chunk = {g.shorter, g.longer, 1.f / (float)g.shorter, tall};
+  float v[kApply / 4];
+  chunk.load(d.u, part * kApply, v);
+  // the entries of a run of lanes lie side by side in the parameter
+  const int i0 = (tall ? threadIdx.x & 15 : threadIdx.x >> 4) * 4, j0 = (tall ? threadIdx.x >> 4 : threadIdx.x & 15) * 2;
+  auto place = [&](int i, int j, size_t& at) {
+    i += i0; j += part * kApply + j0;
+    at = tall ? (size_t)j * g.shorter + i : (size_t)i * g.longer + j;
+    return i < g.shorter && j < g.longer;
+  };
+  float old[4][2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      size_t at;
+      old[i][j] = 0.f;
+      if (place(i, j, at)) old[i][j] = d.bf16 ? bf(static_cast<const uint16_t*>(d.w)[at]) : static_cast<const float*>(d.w)[at];
+    }
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) qs[k * 4 + (threadIdx.x >> 6)][threadIdx.x & 63] = qv[k];
+  chunk.park(v, inv, us);
+  __syncthreads();
+  float acc[4][2] = {};
+#pragma unroll 8
+  for (int k = 0; k < g.shorter; ++k) {
+    const f32x4 qi = *reinterpret_cast<const f32x4*>(&qs[k][i0]);
+    const float2 uj = *reinterpret_cast<const float2*>(&us[k][j0]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { acc[i][0] += qi[i] * uj.x; acc[i][1] += qi[i] * uj.y; }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      size_t at;
+      if (!place(i, j, at)) continue;
+      const float w = d.keep * old[i][j] - d.step * acc[i][j];
+      if (d.bf16) static_cast<uint16_t*>(d.w)[at] = bf16_round(w);
+      else static_cast<float*>(d.w)[at] = w;
+    }
+}
+
 // ---- plan -----------------------------------------------------------------------------------------------------------
 
 // What a product of `count` matrices in tiles of `tile` takes, in us, from these kernels' times over 1 to 64 matrices of 64 x 64 to 4096 x 4096: rounds of
@@ -824,7 +1103,7 @@ int pick_tile(int mode, int planes, int pad, const Sizes& groups, int n, double*
 }
 
 struct Plan {
-  struct G { int planes, shorter, longer, pad, mp, np, count = 0, first = 0; size_t x[2], a, b; float sigma; };   // matrices of one shape and type
+  struct G { int planes, shorter, longer, pad, mp, np, count = 0, first = 0; size_t x[2], a, b, partial, q; float sigma; bool narrow; };   // matrices of one shape and type
   std::vector<G> groups;
   std::vector<int> group_of_tensor, first_of_tensor, parts;
   std::vector<size_t> u, partial;
@@ -839,6 +1118,11 @@ long long parts_of(long long numel, long long* chunk) {
   return (numel + c - 1) / c;
 }
 
+int narrow_tiles(int shorter) {
+  const int m16 = (shorter + 15) / 16;
+  return m16 * (m16 + 1) / 2;
+}
+
 void pad_to(Plan::G& g, int pad) {
   g.pad = pad;
   g.mp = (g.shorter + pad - 1) / pad * pad;
@@ -851,7 +1135,7 @@ double step_cost(const std::vector<Plan::G>& groups, int planes) {
   for (int pad = 64; pad <= largest_tile(planes); pad *= 2) {
     std::vector<Plan::G> some;
     for (const auto& g : groups)
-      if (g.planes == planes && g.pad == pad) some.push_back(g);
+      if (g.planes == planes && g.pad == pad && !g.narrow) some.push_back(g);
     if (some.empty()) continue;
     for (int mode : {kGram, kPoly, kUpdate}) {
       double cost;
@@ -917,6 +1201,7 @@ Plan make_plan(const MuonTensor* t, int n) {
   }
   int first = 0;
   for (auto& g : p.groups) { g.first = first; first += g.count; }
+  for (auto& g : p.groups) g.narrow = g.shorter <= kNarrow && g.longer <= kNarrowLong && g.count <= kNarrowCount;
   for (int planes = 1; planes <= 2; ++planes) choose_padding(p.groups, planes);
   p.matrices = take(sizeof(Matrix) * (size_t)p.n_matrices);
   for (int i = 0; i < n; ++i) {
@@ -931,6 +1216,10 @@ Plan make_plan(const MuonTensor* t, int n) {
   for (auto& g : p.groups) {
     const size_t x = (size_t)g.count * g.planes * g.mp * g.np * 2, a = (size_t)g.count * g.planes * g.mp * g.mp * 2;
     g.x[0] = take(x); g.x[1] = take(x); g.a = take(a); g.b = take(a);
+    if (g.narrow) {   // (many steps take the other way)
+      g.partial = take((size_t)g.count * kMaxSlices * narrow_tiles(g.shorter) * 256 * sizeof(double));
+      g.q = take((size_t)g.count * ((size_t)g.shorter * g.shorter + 1) * sizeof(float));
+    }
     // a power of two that brings entries of the size a flat matrix of norm 1 has to about 1
     g.sigma = std::exp2((float)std::min(14, (int)std::lround(0.5 * std::log2((double)g.mp * g.np))));
   }
@@ -987,6 +1276,30 @@ hipError_t product(Groups& t, int pad, hipStream_t s) {
     if (tile == 128) return launch_product<MODE, 2, 128, 2, 2, 2>(t, blocks, s);
     return launch_product<MODE, 2, 64, 4, 2, 2>(t, blocks, s);
   }
+}
+
+hipError_t narrow_steps(NarrowGroups t, int steps, hipStream_t s) {
+  size_t chain_lds = 0;
+  auto lay_out = [&](auto per_matrix) {
+    long long blocks = 0;
+    for (int i = 0; i < t.n; ++i) {
+      t.g[i].first_block = (int)blocks;
+      blocks += (long long)per_matrix(t.g[i]) * t.g[i].count;
+      chain_lds = std::max(chain_lds, narrow_lds((t.g[i].shorter + 15) / 16));
+    }
+    return dim3((unsigned)blocks);   // at most kMaxGroups * kNarrowCount * kNarrowLong / kApply
+  };
+  dim3 blocks = lay_out([](const NarrowGroup& g) { return g.slices; });
+  hipLaunchKernelGGL(narrow_gram_kernel, blocks, dim3(kThreads), 0, s, t);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  blocks = lay_out([](const NarrowGroup&) { return 1; });
+  if (chain_lds > 64 * 1024)
+    if (hipError_t e = raise_lds_limit(reinterpret_cast<const void*>(narrow_chain_kernel), narrow_lds(kNarrow / 16)); e != hipSuccess) return e;
+  hipLaunchKernelGGL(narrow_chain_kernel, blocks, dim3(kChainThreads), chain_lds, s, t, steps);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  blocks = lay_out([](const NarrowGroup& g) { return (g.longer + kApply - 1) / kApply; });
+  hipLaunchKernelGGL(narrow_apply_kernel, blocks, dim3(kThreads), 0, s, t);
+  return hipGetLastError();
 }
 
 template <int PLANES>
@@ -1048,6 +1361,21 @@ hipError_t launch_muon_step(const MuonTensor* tensors, int n, const spb_muon_con
     hipLaunchKernelGGL(update_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, tab);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
+  const bool few_steps = c.ns_steps <= kNarrowSteps;
+  for (size_t k = 0; few_steps && k < p.groups.size();) {
+    NarrowGroups t = {};
+    for (; k < p.groups.size() && t.n < kMaxGroups; ++k) {
+      const Plan::G& s = p.groups[k];
+      if (!s.narrow) continue;
+      NarrowGroup& d = t.g[t.n++];
+      d.matrices = matrices + s.first;
+      d.partial = reinterpret_cast<double*>(ws + s.partial); d.q = reinterpret_cast<float*>(ws + s.q);
+      d.shorter = s.shorter; d.longer = s.longer; d.count = s.count; d.tiles = narrow_tiles(s.shorter);
+      d.slices = std::min((s.longer + 127) / 128, kMaxSlices);
+    }
+    if (t.n == 0) break;
+    if (hipError_t e = narrow_steps(t, c.ns_steps, stream); e != hipSuccess) return e;
+  }
   for (int planes = 1; planes <= 2; ++planes)
     for (int pad = 64; pad <= largest_tile(planes); pad *= 2) {
       size_t k = 0;
@@ -1055,7 +1383,7 @@ hipError_t launch_muon_step(const MuonTensor* tensors, int n, const spb_muon_con
         Groups t = {};
         for (; k < p.groups.size() && t.n < kMaxGroups; ++k) {
           const Plan::G& s = p.groups[k];
-          if (s.planes != planes || s.pad != pad) continue;
+          if (s.planes != planes || s.pad != pad || (s.narrow && few_steps)) continue;
           Group& d = t.g[t.n++];
           d.x[0] = reinterpret_cast<_Float16*>(ws + s.x[0]); d.x[1] = reinterpret_cast<_Float16*>(ws + s.x[1]);
           d.a = reinterpret_cast<_Float16*>(ws + s.a); d.b = reinterpret_cast<_Float16*>(ws + s.b);

@@ -114,6 +114,14 @@ MATRICES = {
     "stem": dict(shape=(64, 7, 7, 3), blocks=1, workers=2),
     "conv": dict(shape=(96, 3, 3, 24), blocks=1, workers=1),
     "vector": dict(shape=(150,), blocks=1, workers=1),
+    "narrow_16": dict(shape=(16, 1000), blocks=1, workers=2, rank=3),
+    "narrow_33": dict(shape=(5 * 33, 130), blocks=5, workers=1),
+    "narrow_48_long": dict(shape=(48, 8192), blocks=1, workers=1, rank=2),
+    "narrow_48_longer": dict(shape=(8200, 48), blocks=1, workers=1, rank=2),
+    "beyond_narrow": dict(shape=(300, 49), blocks=1, workers=1, rank=2),
+    "narrow_48_tall": dict(shape=(2, 777, 48), blocks=2, workers=3),
+    "many_narrow": dict(shape=(257, 8, 24), blocks=257, workers=1),
+    "most_narrow": dict(shape=(256, 20, 24), blocks=256, workers=1),
 }
 
 
@@ -139,6 +147,19 @@ def test_settings(patch, dtype):
     before = _numpy({k: v for k, v in t.items() if k != "rate_scale"})
     _step([t], hyper)
     _check(before, _numpy({k: v for k, v in t.items() if k != "rate_scale"}), dtype, hyper, 0.75)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shape", [(48, 150), (150, 33), (17, 17), (1, 9)])
+def test_a_short_side_in_one_and_in_many_products(shape, dtype):
+    """Up to 8 steps run on the small Gram matrix, more as products of the whole: both against the formula, whose 8 and 9 steps differ."""
+    for steps in (1, 2, 3, 8, 9, 16):
+        hyper = {**HYPER, "ns_steps": steps}
+        t = _tensor(shape, 1, dtype, 2, seed=12, w=0.0)
+        before = _numpy(t)
+        _step([t], hyper)
+        _check(before, _numpy(t), dtype, hyper)
 
 
 @pytest.mark.gpu
