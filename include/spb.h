@@ -352,7 +352,8 @@ typedef struct spb_muon_tensor {
   double rate_scale;           /* >= 0 */
   int32_t count;               /* 1..SPB_MAX_WORKERS */
   int32_t dtype;               /* of w */
-  int32_t blocks;              /* 0: AdamW; >= 1: matrices of rows / blocks by cols, each side at most SPB_MAX_MATRIX_SIDE */
+  int32_t blocks;              /* 0: AdamW; >= 1: matrices of rows / blocks by cols, each side at most SPB_MAX_MATRIX_SIDE.  A tensor has at most
+                                  2^33 entries, and so have all matrices of a call with their sides rounded up to multiples of 256 */
   int32_t reserved;            /* 0 */
 } spb_muon_tensor;
 #define SPB_MAX_MATRIX_SIDE 65536

@@ -198,57 +198,59 @@ __global__ __launch_bounds__(kThreads) void heads_forward_kernel(Args a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   Token* tok = reinterpret_cast<Token*>(lds);
   float2* cs = reinterpret_cast<float2*>(lds + sizeof(Token) * kMaxTokensPerBlock);
-  const unsigned first = blockIdx.x * (unsigned)a.tokens_per_block;
-  const int n = min(a.tokens_per_block, a.tokens - (int)first);
-  load_tokens(a, first, n, tok, cs);
-  __syncthreads();
   const int l = threadIdx.x % G, chunks = a.dim / V;
   const int rotated = 2 * a.pairs / V, half = a.pairs ? rotated / 2 : chunks / 2;
   int c0, c1;
   chunks_of(l, half, a.interleaved, c0, c1);
   const bool has0 = c0 < chunks, has1 = c1 < chunks;
   const float inv_dim = 1.f / (float)a.dim;
-  for (int g = 0; g < (a.norm ? 2 : 1); ++g) {
-    const int heads = !a.norm ? a.heads : g ? a.heads - a.heads_q : a.heads_q, h0 = g ? a.heads_q : 0, rows = n * heads;
-    if (rows == 0) break;
-    const float inv_heads = 1.f / (float)heads;
-    auto request = [&](int r) {
-      int k, h;
-      place_of(min(r, rows - 1), heads, inv_heads, k, h);
-      return load_pair<T, V>(static_cast<const T*>(a.x) + tok[k].x + (h0 + h) * a.xs[2], c0, c1, has0, has1);
-    };
-    Pair<T, V> next = request(threadIdx.x / G), gam = {}, bet = {};
-    if (a.norm) {
-      gam = load_pair<T, V>(static_cast<const T*>(a.gamma) + g * a.dim, c0, c1, has0, has1);
-      if (a.beta) bet = load_pair<T, V>(static_cast<const T*>(a.beta) + g * a.dim, c0, c1, has0, has1);
-    }
-    for (int r = threadIdx.x / G; r < rows; r += S) {
-      int k, h;
-      place_of(r, heads, inv_heads, k, h);
-      h += h0;
-      const Pair<T, V> now = next;
-      next = request(r + S);
-      if (a.keep) store_pair<T, V>(static_cast<T*>(a.keep) + ((size_t)(first + k) * a.heads + h) * a.dim, now, c0, c1, has0, has1);
-      float u[V], v[V];
-      Chunk<T, V>::unpack(now.c[0], u);
-      Chunk<T, V>::unpack(now.c[1], v);
+  for (unsigned first = blockIdx.x * (unsigned)a.tokens_per_block; first < (unsigned)a.tokens; first += gridDim.x * (unsigned)a.tokens_per_block) {
+    const int n = min(a.tokens_per_block, a.tokens - (int)first);
+    if (first != blockIdx.x * (unsigned)a.tokens_per_block) __syncthreads();   // the last block's angles are done with
+    load_tokens(a, first, n, tok, cs);
+    __syncthreads();
+    for (int g = 0; g < (a.norm ? 2 : 1); ++g) {
+      const int heads = !a.norm ? a.heads : g ? a.heads - a.heads_q : a.heads_q, h0 = g ? a.heads_q : 0, rows = n * heads;
+      if (rows == 0) break;
+      const float inv_heads = 1.f / (float)heads;
+      auto request = [&](int r) {
+        int k, h;
+        place_of(min(r, rows - 1), heads, inv_heads, k, h);
+        return load_pair<T, V>(static_cast<const T*>(a.x) + tok[k].x + (h0 + h) * a.xs[2], c0, c1, has0, has1);
+      };
+      Pair<T, V> next = request(threadIdx.x / G), gam = {}, bet = {};
       if (a.norm) {
-        const float rstd = centre<G>(u, v, has0, has1, inv_dim, a.eps);
-        float w[V], z[V];
-        Chunk<T, V>::unpack(gam.c[0], w);
-        Chunk<T, V>::unpack(bet.c[0], z);
-#pragma unroll
-        for (int e = 0; e < V; ++e) u[e] = w[e] * (u[e] * rstd) + z[e];
-        Chunk<T, V>::unpack(gam.c[1], w);
-        Chunk<T, V>::unpack(bet.c[1], z);
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = w[e] * (v[e] * rstd) + z[e];
+        gam = load_pair<T, V>(static_cast<const T*>(a.gamma) + g * a.dim, c0, c1, has0, has1);
+        if (a.beta) bet = load_pair<T, V>(static_cast<const T*>(a.beta) + g * a.dim, c0, c1, has0, has1);
       }
-      if (a.pairs) turn(u, v, cs + k * a.pairs, c0, c1, rotated, a.interleaved);
-      Pair<T, V> out;
-      out.c[0] = Chunk<T, V>::pack(u);
-      out.c[1] = Chunk<T, V>::pack(v);
-      store_pair<T, V>(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], out, c0, c1, has0, has1);
+      for (int r = threadIdx.x / G; r < rows; r += S) {
+        int k, h;
+        place_of(r, heads, inv_heads, k, h);
+        h += h0;
+        const Pair<T, V> now = next;
+        next = request(r + S);
+        if (a.keep) store_pair<T, V>(static_cast<T*>(a.keep) + ((size_t)(first + k) * a.heads + h) * a.dim, now, c0, c1, has0, has1);
+        float u[V], v[V];
+        Chunk<T, V>::unpack(now.c[0], u);
+        Chunk<T, V>::unpack(now.c[1], v);
+        if (a.norm) {
+          const float rstd = centre<G>(u, v, has0, has1, inv_dim, a.eps);
+          float w[V], z[V];
+          Chunk<T, V>::unpack(gam.c[0], w);
+          Chunk<T, V>::unpack(bet.c[0], z);
+#pragma unroll
+          for (int e = 0; e < V; ++e) u[e] = w[e] * (u[e] * rstd) + z[e];
+          Chunk<T, V>::unpack(gam.c[1], w);
+          Chunk<T, V>::unpack(bet.c[1], z);
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[e] = w[e] * (v[e] * rstd) + z[e];
+        }
+        if (a.pairs) turn(u, v, cs + k * a.pairs, c0, c1, rotated, a.interleaved);
+        Pair<T, V> out;
+        out.c[0] = Chunk<T, V>::pack(u);
+        out.c[1] = Chunk<T, V>::pack(v);
+        store_pair<T, V>(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], out, c0, c1, has0, has1);
+      }
     }
   }
 }
@@ -330,16 +332,16 @@ __global__ __launch_bounds__(kThreads) void heads_norm_backward_kernel(Args a) {
       store_pair<T, V>(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], out, c0, c1, has0, has1);
     }
   }
-  // [lane groups][2][dim] floats.  A column's lane groups are added up by as many threads as there are columns for, each a stretch of
+  // [lane groups][2][dim] floats, rows 16 bytes further apart than that, so that the lane groups of a wavefront write to different banks.  A column's lane groups are added up by as many threads as there are columns for, each a stretch of
   // them in order, and the stretches in order.
   float* sums = reinterpret_cast<float*>(lds);
   __shared__ float part[kThreads];
-  const int columns = 2 * a.dim, width = (int)gridDim.y * a.dim, slot = threadIdx.x / G;
+  const int columns = 2 * a.dim, pitch = columns + 4, width = (int)gridDim.y * a.dim, slot = threadIdx.x / G;
   int stretches = 1;
   while (stretches < S && 2 * stretches * columns <= kThreads) stretches *= 2;
   const int per = S / stretches;
   __syncthreads();
-  float* mine = sums + slot * columns;
+  float* mine = sums + slot * pitch;
 #pragma unroll
   for (int e = 0; e < V; ++e) {
     if (has0) { mine[c0 * V + e] = dgam[0][e]; mine[a.dim + c0 * V + e] = dbet[0][e]; }
@@ -354,7 +356,7 @@ __global__ __launch_bounds__(kThreads) void heads_norm_backward_kernel(Args a) {
     for (int c = threadIdx.x; c < columns; c += kThreads) {
       float s = 0.f;
 #pragma unroll 8
-      for (int i = 0; i < S; ++i) s += sums[i * columns + c];
+      for (int i = 0; i < S; ++i) s += sums[i * pitch + c];
       file(c, s);
     }
   } else {
@@ -362,7 +364,7 @@ __global__ __launch_bounds__(kThreads) void heads_norm_backward_kernel(Args a) {
     float s = 0.f;
     if (stretch < stretches) {
 #pragma unroll 8
-      for (int i = 0; i < per; ++i) s += sums[(stretch * per + i) * columns + c];
+      for (int i = 0; i < per; ++i) s += sums[(stretch * per + i) * pitch + c];
     }
     part[threadIdx.x] = s;
     __syncthreads();
@@ -441,32 +443,34 @@ __global__ __launch_bounds__(kThreads) void heads_forward_any_kernel(Args a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   Token* tok = reinterpret_cast<Token*>(lds);
   float2* cs = reinterpret_cast<float2*>(lds + sizeof(Token) * kMaxTokensPerBlock);
-  const unsigned first = blockIdx.x * (unsigned)a.tokens_per_block;
-  const int n = min(a.tokens_per_block, a.tokens - (int)first);
-  load_tokens(a, first, n, tok, cs);
-  __syncthreads();
   const int lane = threadIdx.x & 63;
   Places at;
   at.init(lane, a.dim, a.pairs, a.interleaved);
   const float inv_dim = 1.f / (float)a.dim;
-  for (int r = threadIdx.x >> 6; r < n * a.heads; r += kThreads / 64) {
-    const int k = r / a.heads, h = r - k * a.heads;
-    Row x;
-    load_row(static_cast<const T*>(a.x) + tok[k].x + h * a.xs[2], at, x);
-    if (a.keep) store_row(static_cast<T*>(a.keep) + ((size_t)(first + k) * a.heads + h) * a.dim, at, x);
-    if (a.norm) {
-      const float rstd = centre_row(at, x, inv_dim, a.eps);
-      const int row = (h >= a.heads_q) * a.dim;
-      Row w;
-      load_row(static_cast<const T*>(a.gamma) + row, at, w);
-      each(at, x, w, [&](float& v, float g, bool) { v = g * (v * rstd); });
-      if (a.beta) {
-        load_row(static_cast<const T*>(a.beta) + row, at, w);
-        each(at, x, w, [&](float& v, float b, bool) { v += b; });
+  for (unsigned first = blockIdx.x * (unsigned)a.tokens_per_block; first < (unsigned)a.tokens; first += gridDim.x * (unsigned)a.tokens_per_block) {
+    const int n = min(a.tokens_per_block, a.tokens - (int)first);
+    if (first != blockIdx.x * (unsigned)a.tokens_per_block) __syncthreads();
+    load_tokens(a, first, n, tok, cs);
+    __syncthreads();
+    for (int r = threadIdx.x >> 6; r < n * a.heads; r += kThreads / 64) {
+      const int k = r / a.heads, h = r - k * a.heads;
+      Row x;
+      load_row(static_cast<const T*>(a.x) + tok[k].x + h * a.xs[2], at, x);
+      if (a.keep) store_row(static_cast<T*>(a.keep) + ((size_t)(first + k) * a.heads + h) * a.dim, at, x);
+      if (a.norm) {
+        const float rstd = centre_row(at, x, inv_dim, a.eps);
+        const int row = (h >= a.heads_q) * a.dim;
+        Row w;
+        load_row(static_cast<const T*>(a.gamma) + row, at, w);
+        each(at, x, w, [&](float& v, float g, bool) { v = g * (v * rstd); });
+        if (a.beta) {
+          load_row(static_cast<const T*>(a.beta) + row, at, w);
+          each(at, x, w, [&](float& v, float b, bool) { v += b; });
+        }
       }
+      if (a.pairs) turn_row(x, at, cs + k * a.pairs, lane);
+      store_row(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], at, x);
     }
-    if (a.pairs) turn_row(x, at, cs + k * a.pairs, lane);
-    store_row(static_cast<T*>(a.out) + tok[k].o + h * a.os[2], at, x);
   }
 }
 
@@ -536,6 +540,7 @@ struct Route {
 // A backward pass with norm takes at most 512 workgroups a kind of head, which walk over the blocks and keep their sums: 16384 tokens of 32 heads of
 // 128: 91 us, with 256 122, with 1024 98; and the 512 partial rows take 4 us to add up.
 constexpr long long kBackwardBlocks = 512;
+constexpr long long kMostBlocks = 1 << 20;   // a grid has fewer than 2^32 threads
 
 Route route_of(const HeadsProblem& q, bool sums) {
   Route r;
@@ -560,12 +565,13 @@ Route route_of(const HeadsProblem& q, bool sums) {
   r.tokens_per_block = tokens_for(sums ? q.heads_q : q.heads_q + q.heads_k);
   if (sums && q.heads_k) r.tokens_per_block_k = tokens_for(q.heads_k);
   r.blocks = (tokens + r.tokens_per_block - 1) / r.tokens_per_block;
+  r.blocks = std::min(r.blocks, kMostBlocks);   // workgroups walk over the rest
   if (sums) {
     r.blocks = std::min(r.blocks, kBackwardBlocks);
     r.kinds = q.heads_k ? 2 : 1;
   }
   r.lds = sizeof(Token) * kMaxTokensPerBlock + sizeof(float2) * (size_t)std::max(r.tokens_per_block, r.tokens_per_block_k) * q.pairs;
-  if (sums) r.lds = std::max(r.lds, (size_t)at_once * 2 * q.head_dim * sizeof(float));
+  if (sums) r.lds = std::max(r.lds, (size_t)at_once * (2 * q.head_dim + 4) * sizeof(float));
   return r;
 }
 

@@ -1237,13 +1237,15 @@ hipError_t launch_product(const Groups& t, int blocks, hipStream_t s) {
   return hipGetLastError();
 }
 
+constexpr long long kMostBlocks = 1 << 23;   // of a launch: a grid has fewer than 2^32 threads
+
 // Lays the workgroups of a launch out over the groups; the number of them, or -1 if it is too large for one.
 template <class F>
 int lay_out(Groups& t, F&& per_matrix) {
   long long blocks = 0;
   for (int i = 0; i < t.n; ++i) {
     const long long per = per_matrix(t.g[i]);
-    if (blocks + per * t.g[i].count > 0x7FFFFFFFll) return -1;
+    if (blocks + per * t.g[i].count > kMostBlocks) return -1;   // (a caller with so many has been refused before)
     t.g[i].first_block = (int)blocks;
     t.g[i].per_matrix = (int)per;
     blocks += per * t.g[i].count;
@@ -1333,30 +1335,30 @@ hipError_t launch_muon_step(const MuonTensor* tensors, int n, const spb_muon_con
     tab.beta1 = (float)c.beta1; tab.beta2 = (float)c.beta2; tab.new1 = (float)(1.0 - c.beta1); tab.new2 = (float)(1.0 - c.beta2);
     tab.inv_c1 = (float)(1.0 / (1.0 - std::pow(c.beta1, (double)c.step)));
     tab.inv_c2 = (float)(1.0 / (1.0 - std::pow(c.beta2, (double)c.step)));
-    int blocks = 0;
+    long long blocks = 0;
     for (; i < n && tab.n < kMaxTensors; ++i) {
       const MuonTensor& s = tensors[i];
-      Tensor& d = tab.t[tab.n++];
       const bool matrix = s.blocks > 0;
+      long long chunk = kPiece;
+      const long long numel = s.rows * s.cols / (matrix ? s.blocks : 1);
+      const long long parts = matrix ? parts_of(numel, &chunk) : (numel + kPiece - 1) / kPiece;
+      if (blocks && blocks + parts * (matrix ? s.blocks : 1) > kMostBlocks) break;
+      Tensor& d = tab.t[tab.n++];
       d.w = s.w; d.m = s.m; d.v = s.v; d.count = s.count; d.bf16 = s.dtype == DType::BF16; d.rate = (float)s.rate; d.keep = (float)(1.0 - s.rate * c.weight_decay);
       d.blocks = matrix ? s.blocks : 1;
-      d.numel = s.rows * s.cols / d.blocks;
+      d.numel = numel; d.parts = (int)parts; d.chunk = chunk;
       d.rows = (int)(matrix ? s.rows / s.blocks : 0); d.cols = (int)(matrix ? s.cols : 0);
-      d.first_block = blocks;
+      d.first_block = (int)blocks;
       uintptr_t bits = (uintptr_t)s.w | (uintptr_t)s.m | (uintptr_t)s.v;
       for (int j = 0; j < s.count; ++j) { d.g[j] = s.g[j]; bits |= (uintptr_t)s.g[j]; }
       d.vector = (bits & 15) == 0 && d.numel % 4 == 0;
       if (matrix) {
-        d.parts = (int)parts_of(d.numel, &d.chunk);
         d.u = reinterpret_cast<float*>(ws + p.u[i]);
         d.partial = reinterpret_cast<double*>(ws + p.partial[i]);
         d.out = matrices + p.first_of_tensor[i];
         d.step = (float)(s.rate * c.rms * std::sqrt((double)std::max(d.rows, d.cols)));
-      } else {
-        d.chunk = kPiece;
-        d.parts = (int)((d.numel + kPiece - 1) / kPiece);
       }
-      blocks += d.parts * d.blocks;
+      blocks += parts * d.blocks;
     }
     hipLaunchKernelGGL(update_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, tab);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;

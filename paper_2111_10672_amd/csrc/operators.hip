@@ -51,7 +51,7 @@ int check_heads(const spb_heads_desc* d, const char* who) {
 int check_strides(const spb_heads_desc* d, const int64_t* s, bool result, const char* name, const char* who) {
   const long long extent[3] = {d->batch, d->seq, (long long)d->heads_q + d->heads_k};
   for (int i = 0; i < 3; ++i)
-    SPB_REQUIRE(s[i] >= 0 && s[i] <= (1ll << 40), SPB_ERR_INVALID_ARG, "%s: stride %lld of %s", who, (long long)s[i], name);
+    SPB_REQUIRE(s[i] >= 0 && (__int128)s[i] * extent[i] <= ((__int128)1 << 60), SPB_ERR_INVALID_ARG, "%s: stride %lld of %s", who, (long long)s[i], name);
   if (!result) return SPB_OK;
   int order[3] = {0, 1, 2};
   std::sort(order, order + 3, [&](int a, int b) { return s[a] < s[b]; });
@@ -92,8 +92,10 @@ int check_config(const spb_muon_config* c, const char* who) {
   return SPB_OK;
 }
 
+constexpr long long kMostEntries = 1ll << 33;   // of a tensor, and of all matrices of a call, padded: the grids behind them count their threads in 32 bits
+
 int check_shape(long long rows, long long cols, int blocks, const char* name, const char* who) {
-  SPB_REQUIRE(rows >= 1 && cols >= 1 && rows <= (1ll << 40) / cols, SPB_ERR_INVALID_ARG, "%s: %s is %lld x %lld", who, name, rows, cols);
+  SPB_REQUIRE(rows >= 1 && cols >= 1 && rows <= kMostEntries / cols, SPB_ERR_INVALID_ARG, "%s: %s is %lld x %lld", who, name, rows, cols);
   SPB_REQUIRE(blocks >= 0, SPB_ERR_INVALID_ARG, "%s: %d blocks of %s", who, blocks, name);
   if (blocks == 0) return SPB_OK;
   SPB_REQUIRE(rows % blocks == 0, SPB_ERR_INVALID_ARG, "%s: %lld rows of %s do not divide into %d blocks", who, rows, name, blocks);
@@ -110,6 +112,10 @@ int check_workspace(const void* workspace, size_t bytes, size_t need, const char
 }
 
 int check_tensors(const std::vector<spb::MuonTensor>& t, const char* who) {
+  __int128 padded = 0;
+  for (const auto& x : t)
+    if (x.blocks) padded += (__int128)x.blocks * ((x.rows / x.blocks + 255) / 256 * 256) * ((x.cols + 255) / 256 * 256);
+  SPB_REQUIRE(padded <= kMostEntries, SPB_ERR_INVALID_ARG, "%s: too many matrices for one call", who);
   std::vector<const void*> seen;
   for (const auto& x : t) seen.push_back(x.w);
   std::sort(seen.begin(), seen.end());

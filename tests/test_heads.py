@@ -285,6 +285,25 @@ def test_no_tokens(b, s):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dim,layout", [(2, "tokens"), (3, "tokens")])
+def test_more_tokens_than_workgroups(dim, layout):
+    """2^24 + 5 tokens of one head, past the 2^20 workgroups of 16 tokens: the last ones as the first."""
+    n, tail = 2 ** 24 + 5, 1000
+    x = torch.randn(1, n, 1, dim, device="cuda").to(torch.bfloat16)
+    rotary = spb.spb_rotary_sections([1])
+    pos = (torch.arange(n, device="cuda", dtype=torch.int32) % 1000).view(1, 1, n)
+    y = torch.zeros_like(x)
+    desc = spb.heads_desc(x, 1, y=y, rotary=rotary)
+    spb.spb_heads_forward(desc, x, y, pos, None, None, torch.cuda.current_stream().cuda_stream)
+    for at in (0, n - tail):
+        part = x[:, at:at + tail].contiguous()
+        want = torch.zeros_like(part)
+        spb.spb_heads_forward(spb.heads_desc(part, 1, rotary=rotary), part, want, pos[:, :, at:at + tail].contiguous(), None, None, torch.cuda.current_stream().cuda_stream)
+        assert torch.equal(y[:, at:at + tail], want)
+    assert (y != 0).any(-1).sum() >= n - 100
+
+
+@pytest.mark.gpu
 def test_offsets_beyond_32_bits():
     """Two sequences 2^31 + 64 elements apart."""
     gap = 2 ** 31 + 64
@@ -322,7 +341,7 @@ def _desc(**patch):
 
 @pytest.mark.parametrize("patch", [dict(dtype=2), dict(batch=-1), dict(batch=65536, seq=32768), dict(heads_q=0), dict(heads_k=-1), dict(head_dim=0), dict(head_dim=257),
                                    dict(eps=0.0), dict(eps=float("nan")), dict(norm=0, r_pairs=0), dict(r_pairs=9), dict(r_pairs=-1), dict(r_axes=0), dict(r_axes=5),
-                                   dict(r_axis=(2, 2)), dict(r_axis=(0, -1)), dict(r_freq=(1, float("inf"))), dict(x_stride=[-64, 64, 16]), dict(y_stride=[192, 64, 15]),
+                                   dict(r_axis=(2, 2)), dict(r_axis=(0, -1)), dict(r_freq=(1, float("inf"))), dict(x_stride=[-64, 64, 16]), dict(x_stride=[1 << 60, 64, 16]), dict(y_stride=[192, 64, 15]),
                                    dict(y_stride=[192, 48, 16]), dict(y_stride=[0, 64, 16]), dict(y_stride=[128, 64, 16])])
 def test_descriptions_that_are_refused(patch):
     with pytest.raises(spb.SpbError) as e:
