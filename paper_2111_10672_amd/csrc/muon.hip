@@ -32,7 +32,10 @@ using gemm_detail::u32x4;
 using gemm_detail::xcd_tile;
 using gemm_dma_detail::krow_rot;
 using gemm_dma_detail::wait_loads_and_barrier;
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4_t;
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr int kThreads = 256;
@@ -439,7 +442,6 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(Groups 
   using SourceQ = Panel<BT, LQ, NW>;
   constexpr int kLoads = 2 * PLANES * SourceP::kInstr;
   static_assert((STAGES - 2) * kLoads < 64, "vmcnt range");
-  static_assert((size_t)NW * 32 * (WN + 4) * 4 <= (size_t)STAGES * kStageBytes, "epilogue staging fits in the ring");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   int mat, tile;
   const Group& g = group_of<false>(groups, xcd_tile(blockIdx.x, gridDim.x), mat, tile);
@@ -510,37 +512,6 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(Groups 
     else if constexpr (R < kReads) fq[S][R - PLANES * TM] = ReaderQ::template read<(R - PLANES * TM) % TN, KG>(where.q[(R - PLANES * TM) / TN]);
   };
 
-  // What 32 rows of the wave's tile are combined with - kPoly: entries of A, kFinal: the parameter's - is requested one strip ahead, the first here.
-  constexpr int LD = WN + 4, kUnits = WN / 16;         // units of 8 entries of a lane
-  const Matrix d = MODE == kFinal ? g.matrices[mat] : Matrix{};
-  const bool turn = MODE == kFinal ? d.rows > d.cols : ti != tj;   // a mirror image to write, or a tall parameter
-  u32x4 held[2][kUnits][PLANES];
-  Entries<PLANES> old[2][kUnits];
-  // rows and columns of unit k of strip i: along the rows, and along the columns
-  auto unit = [&](int i, int k, int& row, int& col, int& r, int& c) {
-    r = (k * 64 + lane) / (WN / 8); c = (k * 64 + lane) % (WN / 8) * 8;
-    row = ti * BT + wm * WM + i * 32 + r; col = tj * BT + wn * WN + c;
-  };
-  auto turned = [&](int i, int k, int& row, int& col, int& r, int& c) {
-    c = k * 16 + (lane >> 2); r = (lane & 3) * 8;
-    row = tj * BT + wn * WN + c; col = ti * BT + wm * WM + i * 32 + r;
-  };
-  auto request = [&](int i) {
-    int row, col, r, c;
-#pragma unroll
-    for (int k = 0; k < kUnits; ++k) {
-      if constexpr (MODE == kPoly) {
-        unit(i, k, row, col, r, c);
-#pragma unroll
-        for (int pl = 0; pl < PLANES; ++pl) held[i & 1][k][pl] = *reinterpret_cast<const u32x4*>(a + pl * plane_a + (size_t)row * g.mp + col);
-      } else if constexpr (MODE == kFinal) {
-        if (turn) turned(i, k, row, col, r, c);
-        else unit(i, k, row, col, r, c);
-        request8<PLANES>(d, row, col, old[i & 1][k]);
-      }
-    }
-  };
-  request(0);
 #pragma unroll
   for (int t = 0; t < STAGES - 1; ++t)
 #pragma unroll
@@ -595,60 +566,138 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(Groups 
     });
   }
   wait_loads_and_barrier<0>();   // every wave is done with the ring
-  if constexpr (PLANES == 2) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] += acc_lo[i][j][r] * (1.f / kLoScale);
-  }
-
-  // 32 rows of the wave's tile at a time through its own part of LDS, so that what they are combined with and what they become move in
-  // 16-byte pieces: first row by row, then, for a mirror image or a tall parameter, column by column from what the first left there.
-  float* strip = reinterpret_cast<float*>(lds) + wave * (32 * LD);
+  // What is stored, rounded to its planes in the registers, goes through the wave's own part of LDS, so that it moves in 16-byte pieces: as it
+  // lies, and for a mirror image or a tall parameter transposed by the reads (ds_read_b64_tr_b16: of 4 rows of 16 columns each of 16 lanes gets
+  // a column).  The whole tile at once: 32 rows at a time in float32 were four round trips to LDS, a third of the time of a product over k = 768.
+  constexpr int kRow = WN * 2, kChunks = WN / 8, kPlane = WM * kRow;   // bytes of a row, its 16-byte chunks, bytes of a plane
+  constexpr int kUnits = WM * WN / 512, kBatch = kUnits < 8 ? kUnits : 8;   // pieces of 8 entries of a lane
+  static_assert(NW * PLANES * kPlane <= STAGES * kStageBytes, "the results fit in the ring");
+  char* mine = lds + wave * (PLANES * kPlane);
+  // a row's chunks are permuted by the row, so that the 32 rows of a fragment lie in different banks
+  auto spot = [&](int row, int col) {
+    constexpr int kShift = kChunks == 8 ? 1 : 2;
+    return mine + row * kRow + ((((col >> 3) ^ (row >> kShift)) & (kChunks - 1)) << 4) + (col & 7) * 2;
+  };
   const float inv_sigma = 1.f / g.sigma;
+  const Matrix d = MODE == kFinal ? g.matrices[mat] : Matrix{};
+  const bool turn = MODE == kFinal ? d.rows > d.cols : ti != tj;   // a mirror image to write, or a tall parameter
+  const int row0 = ti * BT + wm * WM, col0 = tj * BT + wn * WN;
+  // piece k of the lane: along the rows, and along the columns
+  auto along_row = [&](int k, int& r, int& c) { r = (k * 64 + lane) / kChunks; c = (k * 64 + lane) % kChunks * 8; };
+  auto along_col = [&](int k, int& r, int& c) { r = k / (WN / 16) * 32 + (lane >> 4) * 8; c = k % (WN / 16) * 16 + (lane & 15); };
+  if constexpr (MODE == kPoly) {   // the entries of A, in the places of what they become part of
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    if (i + 1 < TM) request(i + 1);
+    for (int k0 = 0; k0 < kUnits; k0 += kBatch) {
+      u32x4 in[kBatch][PLANES];
+      int r, c;
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+      for (int k = 0; k < kBatch; ++k) {
+        along_row(k0 + k, r, c);
 #pragma unroll
-      for (int r = 0; r < 16; r += 4)
-        *reinterpret_cast<f32x4*>(strip + (lane & 31) * LD + j * 32 + 2 * r + 4 * (lane >> 5)) = f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
-    gemm_dma_detail::lanes_together();
+        for (int pl = 0; pl < PLANES; ++pl) in[k][pl] = *reinterpret_cast<const u32x4*>(a + pl * plane_a + (size_t)(row0 + r) * g.mp + col0 + c);
+      }
 #pragma unroll
-    for (int k = 0; k < kUnits; ++k) {
-      int row, col, r, c;
-      unit(i, k, row, col, r, c);
-      float* at_s = strip + r * LD + c;
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(at_s), hi = *reinterpret_cast<const f32x4*>(at_s + 4);
-      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      finish8<MODE, PLANES>(v, inv_sigma, held[i & 1][k], row - col);
-      if constexpr (MODE == kGram) split8<PLANES>(v, a + (size_t)row * g.mp + col, plane_a);
-      else if constexpr (MODE == kPoly) split8<PLANES>(v, b + (size_t)row * g.mp + col, plane_a);
-      else if constexpr (MODE == kUpdate) split8<PLANES>(v, g.x[1] + mat * PLANES * plane_x + (size_t)row * g.np + col, plane_x);
-      else if (!turn) apply8<PLANES>(d, inv_sigma, v, row, col, old[i & 1][k]);
-      if (MODE != kUpdate && turn) {
-        *reinterpret_cast<f32x4*>(at_s) = f32x4{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<f32x4*>(at_s + 4) = f32x4{v[4], v[5], v[6], v[7]};
+      for (int k = 0; k < kBatch; ++k) {
+        along_row(k0 + k, r, c);
+#pragma unroll
+        for (int pl = 0; pl < PLANES; ++pl) *reinterpret_cast<u32x4*>(spot(r, c) + pl * kPlane) = in[k][pl];
       }
     }
     gemm_dma_detail::lanes_together();
-    if constexpr (MODE != kUpdate) {
-      if (turn) {   // uniform
+  }
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-          int row, col, r, c;
-          turned(i, k, row, col, r, c);
-          float v[8];
+  for (int i = 0; i < TM; ++i)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = strip[(r + e) * LD + c];
-          if constexpr (MODE == kGram) split8<PLANES>(v, a + (size_t)row * g.mp + col, plane_a);
-          else if constexpr (MODE == kPoly) split8<PLANES>(v, b + (size_t)row * g.mp + col, plane_a);
-          else apply8<PLANES>(d, inv_sigma, v, row, col, old[i & 1][k]);
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int r = i * 32 + (lane & 31), c = j * 32 + 2 * e + 4 * (lane >> 5);
+        char* place = spot(r, c);
+        const float by = MODE == kGram ? kTau * inv_sigma * inv_sigma : MODE == kPoly ? kC / kTau : 1.f / kTau;
+        f32x4 v = f32x4{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+        if constexpr (PLANES == 2) v += f32x4{acc_lo[i][j][e], acc_lo[i][j][e + 1], acc_lo[i][j][e + 2], acc_lo[i][j][e + 3]} * (1.f / kLoScale);
+        v *= by;
+        if constexpr (MODE == kPoly) {
+          f32x4 s = __builtin_convertvector(*reinterpret_cast<const f16x4*>(place), f32x4);
+          if constexpr (PLANES == 2) s += __builtin_convertvector(*reinterpret_cast<const f16x4*>(place + kPlane), f32x4) * (1.f / kLoScale);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[q] += kB * s[q] + (row0 + r == col0 + c + q ? kA * kTau : 0.f);
         }
-        gemm_dma_detail::lanes_together();
+        const f16x4 hi = __builtin_convertvector(v, f16x4);
+        *reinterpret_cast<f16x4*>(place) = hi;
+        if constexpr (PLANES == 2) *reinterpret_cast<f16x4*>(place + kPlane) = __builtin_convertvector((v - __builtin_convertvector(hi, f32x4)) * kLoScale, f16x4);
+      }
+  gemm_dma_detail::lanes_together();
+  // where entry (row, col) of the result lies
+  auto result = [&](int row, int col) -> _Float16* {
+    if constexpr (MODE == kUpdate) return g.x[1] + mat * PLANES * plane_x + (size_t)row * g.np + col;
+    else return (MODE == kGram ? a : b) + (size_t)row * g.mp + col;
+  };
+  constexpr size_t kNone = 0;
+  const size_t plane_out = MODE == kUpdate ? plane_x : MODE == kFinal ? kNone : plane_a;
+  if (MODE != kFinal || !turn) {
+#pragma unroll
+    for (int k0 = 0; k0 < kUnits; k0 += kBatch) {
+      Entries<PLANES> old[kBatch];
+      int r, c;
+      if constexpr (MODE == kFinal) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+          along_row(k0 + k, r, c);
+          request8<PLANES>(d, row0 + r, col0 + c, old[k]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        along_row(k0 + k, r, c);
+        u32x4 w[PLANES];
+#pragma unroll
+        for (int pl = 0; pl < PLANES; ++pl) w[pl] = *reinterpret_cast<const u32x4*>(spot(r, c) + pl * kPlane);
+        if constexpr (MODE == kFinal) {
+          float v[8];
+          join8<PLANES>(w, v);
+          apply8<PLANES>(d, inv_sigma, v, row0 + r, col0 + c, old[k]);
+        } else {
+#pragma unroll
+          for (int pl = 0; pl < PLANES; ++pl) *reinterpret_cast<u32x4*>(result(row0 + r, col0 + c) + pl * plane_out) = w[pl];
+        }
+      }
+    }
+  }
+  if constexpr (MODE != kUpdate) {
+    if (!turn) return;   // uniform over the workgroup
+#pragma unroll
+    for (int k0 = 0; k0 < kUnits; k0 += kBatch) {
+      Entries<PLANES> old[kBatch];
+      int r, c;
+      if constexpr (MODE == kFinal) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+          along_col(k0 + k, r, c);
+          request8<PLANES>(d, col0 + c, row0 + r, old[k]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        along_col(k0 + k, r, c);
+        u32x4 w[PLANES];
+#pragma unroll
+        for (int pl = 0; pl < PLANES; ++pl)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {   // this lane's word: 4 columns of row (lane % 16) / 4 of the 4
+            const char* word = spot(r + 4 * h + ((lane & 15) >> 2), (c & ~15) + 4 * (lane & 3)) + pl * kPlane;
+            const s16x4 got = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(__attribute__((address_space(3))) const char*)word);
+            const uint2 bits = __builtin_bit_cast(uint2, got);
+            w[pl][2 * h] = bits.x; w[pl][2 * h + 1] = bits.y;
+          }
+        if constexpr (MODE == kFinal) {
+          float v[8];
+          join8<PLANES>(w, v);
+          apply8<PLANES>(d, inv_sigma, v, col0 + c, row0 + r, old[k]);
+        } else {
+#pragma unroll
+          for (int pl = 0; pl < PLANES; ++pl) *reinterpret_cast<u32x4*>(result(col0 + c, row0 + r) + pl * plane_out) = w[pl];
+        }
       }
     }
   }
