@@ -238,9 +238,17 @@ __device__ __forceinline__ std::conditional_t<EARLY, Group, const Group&> group_
   }
 }
 
+// A value that is about to be split is rounded to float32 here, once.  Left to itself the compiler contracts the product it comes from with one of the
+// two conversions to float16 and not with the other; next to a tie the stored value and the one the remainder is taken from are then a float16 step apart.
+__device__ __forceinline__ void settle(float& v) { asm volatile("" : "+v"(v)); }
+
 // value and remainder of v at p and, with two planes, p + plane
 template <int PLANES>
-__device__ __forceinline__ void split8(const float (&v)[8], _Float16* p, size_t plane) {
+__device__ __forceinline__ void split8(float (&v)[8], _Float16* p, size_t plane) {
+  if constexpr (PLANES == 2) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) settle(v[e]);
+  }
   f16x8 hi;
 #pragma unroll
   for (int e = 0; e < 8; ++e) hi[e] = (_Float16)v[e];
@@ -622,6 +630,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(Groups 
           if constexpr (PLANES == 2) s += __builtin_convertvector(*reinterpret_cast<const f16x4*>(place + kPlane), f32x4) * (1.f / kLoScale);
 #pragma unroll
           for (int q = 0; q < 4; ++q) v[q] += kB * s[q] + (row0 + r == col0 + c + q ? kA * kTau : 0.f);
+        }
+        if constexpr (PLANES == 2) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float one = v[q];
+            settle(one);
+            v[q] = one;
+          }
         }
         const f16x4 hi = __builtin_convertvector(v, f16x4);
         *reinterpret_cast<f16x4*>(place) = hi;

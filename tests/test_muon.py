@@ -149,6 +149,40 @@ def test_settings(patch, dtype):
     _check(before, _numpy({k: v for k, v in t.items() if k != "rate_scale"}), dtype, hyper, 0.75)
 
 
+# Entry by entry, for the two float16 of a float32 parameter: err bounds |error of X| and grows with every product P Q by |dP| |Q| + |P| |dQ| + chain |P| |Q|, with
+# every matrix stored by 2^-21 of each entry (the remainder x remainder that its products leave out among it) and 2^-40 for entries so small that the remainder,
+# in steps of 2^-35 at sigma or tau times the entry, is short of bits.  A remainder taken from another rounding than that of
+# the stored value is off by a step of float16, 2^-11 of the entry at least, which no later product takes back.
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(64, 4000), (128, 512), (512, 96), (130, 1031)])
+@pytest.mark.parametrize("steps", [1, 2])
+def test_every_entry_of_a_float32_matrix(shape, steps):
+    hyper = dict(HYPER, lr=1.0, rms=1.0 / math.sqrt(max(shape)), momentum=0.0, nesterov=False, ns_steps=steps, weight_decay=0.0)
+    t = _tensor(shape, 1, torch.float32, 1, 77)
+    t["w"].zero_()
+    u = t["grads"][0].double().cpu().numpy()
+    _step([t], hyper)
+    got = -t["w"].double().cpu().numpy()
+    if shape[0] > shape[1]:
+        u, got = u.T, got.T
+    h, tiny = 2.0 ** -21, 2.0 ** -40
+    chain = lambda k: (k / 16 + 16) * U
+    x = u / (np.linalg.norm(u) + hyper["ns_eps"])
+    err = (h + 4 * U) * np.abs(x) + tiny
+    for _ in range(steps):
+        a = x @ x.T
+        off_a = err @ np.abs(x.T) + np.abs(x) @ err.T + chain(x.shape[1]) * np.abs(x) @ np.abs(x.T)
+        stored_a = off_a + h * np.abs(a) + tiny
+        b = -4.7750 * a + 2.0315 * a @ a
+        off_b = 4.7750 * stored_a + 2.0315 * (stored_a @ np.abs(a) + np.abs(a) @ stored_a + chain(len(a)) * np.abs(a) @ np.abs(a)) + 8 * U * np.abs(b)
+        b = b + GROWTH * np.eye(len(a))
+        off_b += h * np.abs(b) + tiny
+        err = off_b @ np.abs(x) + np.abs(b) @ err + chain(len(a)) * np.abs(b) @ np.abs(x)
+        x = b @ x
+        err += (h + 4 * U) * np.abs(x) + tiny
+    assert (np.abs(got - x) <= err).all(), float((np.abs(got - x) / err).max())
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("shape", [(48, 150), (150, 33), (17, 17), (1, 9)])
