@@ -272,8 +272,14 @@ __device__ __forceinline__ void join8(const u32x4 (&w)[PLANES], float (&v)[8]) {
   }
 }
 
-// X = sigma u / (|u| + eps), shorter side first, zeros in the padding.  A workgroup per 64 x 64 entries.
-template <int PLANES>
+// Where entry (row, col) of a matrix of `ld` columns lies in blocks of 16 rows and 32 columns, col a multiple of 8: the 16 bytes of each lane of a wavefront's operand
+// behind one another, so that a wavefront loads an operand as 1 KB in a row, without LDS.
+__device__ __forceinline__ size_t place(int ld, int row, int col) {
+  return ((size_t)(row >> 4) * (ld >> 5) + (col >> 5)) * 512 + (((col >> 3) & 3) * 16 + (row & 15)) * 8;
+}
+
+// X = sigma u / (|u| + eps), shorter side first, zeros in the padding.  A workgroup per 64 x 64 entries.  BLOCKS: X lies as `place` says.
+template <int PLANES, bool BLOCKS>
 __global__ __launch_bounds__(kThreads) void normalise_kernel(Groups groups) {
   __shared__ float tile_s[64][65];
   __shared__ double sums[kThreads / 64];
@@ -311,11 +317,11 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(Groups groups) {
   const size_t plane = (size_t)g.mp * g.np;
   _Float16* x = g.x[0] + mat * PLANES * plane;
   for (int k = threadIdx.x; k < 64 * 8; k += kThreads) {
-    const int i = k >> 3, j = (k & 7) * 8;
+    const int i = BLOCKS ? (k >> 7) * 16 + (k & 15) : k >> 3, j = BLOCKS ? ((k >> 4) & 7) * 8 : (k & 7) * 8;
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = (tall ? tile_s[j + e][i] : tile_s[i][j + e]) * scale;
-    split8<PLANES>(v, x + (size_t)(i0 + i) * g.np + j0 + j, plane);
+    split8<PLANES>(v, x + (BLOCKS ? place(g.np, i0 + i, j0 + j) : (size_t)(i0 + i) * g.np + j0 + j), plane);
   }
 }
 
@@ -852,15 +858,223 @@ __global__ __launch_bounds__(kThreads) void small_product_kernel(Groups groups) 
   }
 }
 
-// ---- matrices with a short side of at most 48 -----------------------------------------------------------------------
+// ---- steps of two launches ------------------------------------------------------------------------------------------
+
+// Matrices of a padded shorter side of at most 256, as long as there are few of them: what a step takes is launches, 3 us and more each whatever they do, and
+// latency.  X and A lie in blocks (`place`), so that operands go from memory to registers.  One step of the optimiser against three launches a step: 4 of 60 x 60 in
+// bfloat16 41 us (60), one of 256 x 784 51 (66), in float32 69 (83), 24 of 128 x 512 in float32 66 (96), 4 of 128 x 4000 in float32 100 (149).
+constexpr int kStrip = 16;                // columns of a workgroup of pair_kernel
+constexpr int kShareThreads = 512;
+
+// A = X X^T in tiles of T x T, those on and below the diagonal; eight wavefronts share the long side and have their next AHEAD pieces of 64 of it in flight.  Their
+// partial tiles are added up in wavefront order.  256 x 784 in float32: 3.8 us, where tiles of 32 through LDS by four wavefronts take 5.9.
+template <int PLANES, int T, int AHEAD>
+__global__ __launch_bounds__(kShareThreads) void share_gram_kernel(Groups groups) {
+  constexpr int NW = kShareThreads / 64, TB = T / 16, LD = T + 4;
+  __shared__ __attribute__((aligned(16))) float parts[NW * T * LD];
+  int mat, tile, ti, tj;
+  const Group g = group_of<true>(groups, xcd_tile(blockIdx.x, gridDim.x), mat, tile);
+  place_tile<kGram>(tile, g.mp / T, ti, tj);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const size_t plane_x = (size_t)g.mp * g.np, plane_a = (size_t)g.mp * g.mp;
+  const int pieces = g.np / 64, first = wave * pieces / NW, n = (wave + 1) * pieces / NW - first;
+  const _Float16* x = g.x[0] + mat * PLANES * plane_x + (size_t)first * 1024 + lane * 8;
+  const _Float16* p = x + (size_t)(ti * TB) * (g.np / 32) * 512;   // the blocks of a row of blocks lie behind one another
+  const _Float16* q = x + (size_t)(tj * TB) * (g.np / 32) * 512;
+  u32x4 fp[AHEAD][2][TB][PLANES], fq[AHEAD][2][TB][PLANES];
+  auto load = [&](auto slot, int u) {
+    constexpr int S = decltype(slot)::value;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < TB; ++i)
+#pragma unroll
+        for (int pl = 0; pl < PLANES; ++pl) {
+          const size_t at = pl * plane_x + (size_t)i * (g.np / 32) * 512 + (size_t)(2 * u + h) * 512;
+          fp[S][h][i][pl] = *reinterpret_cast<const u32x4*>(p + at);
+          fq[S][h][i][pl] = *reinterpret_cast<const u32x4*>(q + at);
+        }
+  };
+  f32x4 acc[TB][TB] = {}, lo[TB][TB] = {};
+  gemm_detail::static_for<AHEAD>([&](auto slot) {
+    if (decltype(slot)::value < n) load(slot, decltype(slot)::value);
+  });
+  for (int u = 0; u < n; u += AHEAD)
+    gemm_detail::static_for<AHEAD>([&](auto slot) {
+      constexpr int S = decltype(slot)::value;
+      if (u + S < n) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < TB; ++i)
+#pragma unroll
+            for (int j = 0; j < TB; ++j) {   // (operands exchanged: a lane then holds four columns of one row)
+              auto mfma = [&](int pq, int pp, f32x4& into) {
+                into = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, fq[S][h][j][pq]), __builtin_bit_cast(f16x8, fp[S][h][i][pp]), into, 0, 0, 0);
+              };
+              mfma(0, 0, acc[i][j]);
+              if constexpr (PLANES == 2) {
+                mfma(1, 0, lo[i][j]);
+                mfma(0, 1, lo[i][j]);
+              }
+            }
+        if (u + S + AHEAD < n) load(slot, u + S + AHEAD);
+      }
+    });
+#pragma unroll
+  for (int i = 0; i < TB; ++i)
+#pragma unroll
+    for (int j = 0; j < TB; ++j) {
+      if constexpr (PLANES == 2) acc[i][j] += lo[i][j] * (1.f / kLoScale);
+      *reinterpret_cast<f32x4*>(&parts[wave * (T * LD) + (16 * i + (lane & 15)) * LD + 16 * j + 4 * (lane >> 4)]) = acc[i][j];
+    }
+  __syncthreads();
+  constexpr int kFinish = T * T / 8;      // threads with 8 entries each
+  const int r = (threadIdx.x & (kFinish - 1)) % T, c = (threadIdx.x & (kFinish - 1)) / T * 8;
+  const float inv_sigma = 1.f / g.sigma;
+  _Float16* a = g.a + mat * PLANES * plane_a;
+  float* at_s = parts + r * LD + c;
+  float v[8];
+  if (threadIdx.x < kFinish) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float sum = at_s[e];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) sum += at_s[w * (T * LD) + e];
+      v[e] = sum * (kTau * inv_sigma * inv_sigma);
+      at_s[e] = v[e];
+    }
+    split8<PLANES>(v, a + place(g.mp, ti * T + r, tj * T + c), plane_a);
+  }
+  if (ti == tj) return;
+  __syncthreads();
+  if (threadIdx.x >= kFinish) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = parts[(c + e) * LD + r];
+  split8<PLANES>(v, a + place(g.mp, tj * T + r, ti * T + c), plane_a);
+}
+
+// The second and third product of a step in one launch: X' = a X + A Z with Z = b X + c A X, for a strip of 16 columns, whose products need nothing of the other
+// strips.  A wavefront has 32 rows; its part of A, the left operand of both products, goes from memory to registers and stays there, and the strip's X and Z
+// lie transposed in LDS, k contiguous.  Z takes the place of B as what is rounded to float16 in between: |Z| <= 2.9 in the spectral norm where X stays
+// below 1.3, so sigma |z| <= 2.9 * 2^14.  Bound by the load of A, 64 bytes a clock into a CU: 256 x 784 in float32 7.6 us, in bfloat16 4.6, and 13 and 7.3 with A in
+// rows, where a quarter of a wavefront's load asks for 16 lines.
+template <bool FINAL, int PLANES, int MP>
+__device__ __forceinline__ void pair_strip(const Group& g, int mat, int strip, char* lds) {
+  constexpr int W = kStrip, LD = MP + 8, LF = MP + 4, STEPS = MP / 32;
+  if (threadIdx.x >= 2 * MP) return;   // whole wavefronts: the workgroup has as many as the largest matrix of the launch needs
+  _Float16* xt = reinterpret_cast<_Float16*>(lds);
+  _Float16* zt = xt + PLANES * W * LD;
+  float* out = reinterpret_cast<float*>(zt + PLANES * W * LD);
+  const int lane = threadIdx.x & 63, row0 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 32, col0 = strip * W;
+  const size_t plane_x = (size_t)MP * g.np;
+  constexpr size_t plane_a = (size_t)MP * MP;
+  const _Float16* x = g.x[0] + mat * PLANES * plane_x;
+  const _Float16* a = g.a + mat * PLANES * plane_a;
+  const Matrix d = FINAL ? g.matrices[mat] : Matrix{};
+  const bool turn = FINAL && d.rows > d.cols;
+  const int row = (threadIdx.x >> 5) * 16 + (threadIdx.x & 15), c = ((threadIdx.x >> 4) & 1) * 8;   // this thread's 8 entries of X and, as they lie, of X'
+  const int tn = threadIdx.x / (MP / 8), tc = threadIdx.x % (MP / 8) * 8;                             // and of a tall parameter
+  u32x4 in[PLANES];
+#pragma unroll
+  for (int pl = 0; pl < PLANES; ++pl) in[pl] = *reinterpret_cast<const u32x4*>(x + pl * plane_x + place(g.np, row, col0 + c));
+  u32x4 fa[2][STEPS][PLANES];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int pl = 0; pl < PLANES; ++pl)   // `place` of row row0 + 16 i + lane % 16, column 32 s + 8 (lane / 16)
+        fa[i][s][pl] = *reinterpret_cast<const u32x4*>(a + pl * plane_a + ((size_t)((row0 >> 4) + i) * STEPS + s) * 512 + lane * 8);
+  Entries<PLANES> old;
+  if (FINAL) request8<PLANES>(d, turn ? col0 + tn : row, turn ? tc : col0 + c, old);
+#pragma unroll
+  for (int pl = 0; pl < PLANES; ++pl) {
+    const f16x8 w = __builtin_bit_cast(f16x8, in[pl]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) xt[pl * W * LD + (c + e) * LD + row] = w[e];
+  }
+  __syncthreads();
+  const int n = lane & 15, kg = lane >> 4;
+  f32x4 acc[2];
+  auto multiply = [&](const _Float16* right) {
+    f32x4 lo[2] = {};
+    acc[0] = acc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      f16x8 q[PLANES];
+#pragma unroll
+      for (int pl = 0; pl < PLANES; ++pl) q[pl] = *reinterpret_cast<const f16x8*>(right + pl * W * LD + n * LD + s * 32 + kg * 8);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const f16x8 p = __builtin_bit_cast(f16x8, fa[i][s][0]);
+        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, q[0], acc[i], 0, 0, 0);
+        if constexpr (PLANES == 2) {
+          lo[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, fa[i][s][1]), q[0], lo[i], 0, 0, 0);
+          lo[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p, q[1], lo[i], 0, 0, 0);
+        }
+      }
+    }
+    if constexpr (PLANES == 2) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) acc[i] += lo[i] * (1.f / kLoScale);
+    }
+  };
+  multiply(xt);
+  f32x4 own[2];   // of X, where this lane has sums
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int at = n * LD + row0 + 16 * i + 4 * kg;
+    own[i] = __builtin_convertvector(*reinterpret_cast<const f16x4*>(xt + at), f32x4);
+    if constexpr (PLANES == 2) own[i] += __builtin_convertvector(*reinterpret_cast<const f16x4*>(xt + W * LD + at), f32x4) * (1.f / kLoScale);
+    f32x4 z;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float one = kB * own[i][q] + kC / kTau * acc[i][q];
+      if constexpr (PLANES == 2) settle(one);
+      z[q] = one;
+    }
+    const f16x4 hi = __builtin_convertvector(z, f16x4);
+    *reinterpret_cast<f16x4*>(zt + at) = hi;
+    if constexpr (PLANES == 2) *reinterpret_cast<f16x4*>(zt + W * LD + at) = __builtin_convertvector((z - __builtin_convertvector(hi, f32x4)) * kLoScale, f16x4);
+  }
+  __syncthreads();
+  multiply(zt);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4*>(out + n * LF + row0 + 16 * i + 4 * kg) = kA * own[i] + acc[i] * (1.f / kTau);
+  __syncthreads();
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = turn ? out[tn * LF + tc + e] : out[(c + e) * LF + row];
+  if constexpr (FINAL) apply8<PLANES>(d, 1.f / g.sigma, v, turn ? col0 + tn : row, turn ? tc : col0 + c, old);
+  else split8<PLANES>(v, g.x[1] + mat * PLANES * plane_x + place(g.np, row, col0 + c), plane_x);
+}
+// MOST: the largest shorter side of the launch.
+template <bool FINAL, int PLANES, int MOST>
+__global__ __launch_bounds__(2 * MOST) void pair_kernel(Groups groups) {
+  __shared__ __attribute__((aligned(16))) char lds[kStrip * (2 * PLANES * 2 * (MOST + 8) + 4 * (MOST + 4))];
+  int mat, strip;
+  const Group g = group_of<true>(groups, xcd_tile(blockIdx.x, gridDim.x), mat, strip);
+  if (g.mp == 64) return pair_strip<FINAL, PLANES, 64>(g, mat, strip, lds);
+  if constexpr (MOST >= 128)
+    if (g.mp == 128) return pair_strip<FINAL, PLANES, 128>(g, mat, strip, lds);
+  if constexpr (MOST >= 256) {
+    if (g.mp == 192) return pair_strip<FINAL, PLANES, 192>(g, mat, strip, lds);
+    return pair_strip<FINAL, PLANES, 256>(g, mat, strip, lds);
+  }
+}
+
+// ---- matrices with a short side of at most 32 or 48 -----------------------------------------------------------------
 
 // The steps' polynomials commute with A = X X^T, so for a matrix of a short side the whole chain can run on that one small matrix: with
 // B_k = a I + b A_k + c A_k^2,  A_{k+1} = A_k B_k^2  and  X_steps = (B_{steps-1} ... B_0) X_0.  That squares singular values, and rounding in A_0 grows
 // up to a^2 = 11.9 times a step where they are small: in float32 too much of it, in float64 at most 1e-16 * 11.9^7 = 3e-9 by the eighth step, which
 // is where it is used.  Three launches in place of three a step: the entries of A in float64 from slices of the long side, one workgroup a matrix
-// for the chain, the product with u and the update.  16 x 100: 26 us a step of the optimiser, 32 x 300 33, 48 x 300 47, where the products of the whole matrix
-// take 58, most of it 17 launches; a short side of 64 took 66 to 86 us this way (the chain 50, bound by one CU's float64 matrix rate and LDS).
-constexpr int kNarrow = 48, kNarrowLong = 8192, kNarrowSteps = 8, kNarrowCount = 256, kMaxSlices = 16, kNarrowTiles = 6;
+// for the chain, the product with u and the update.  The chain is bound by one CU's float64 matrix rate and
+// LDS.  A step of the optimiser, and in brackets as products of the whole matrix: 16 x 100 25 us (41), 32 x 300 33 (42), 16 of 32 x 2000 42 (51), in float32 40 (68); from 33
+// on bfloat16 ones no longer gain (48 x 300: 48 (43)), and float32 ones, whose products are three, about as much as they lose (48 x 300: 47 (45), 16 of 48 x 2000: 59 (71)).
+constexpr int narrow_side(int planes) { return planes == 2 ? 48 : 32; }
+constexpr int kNarrow = narrow_side(2), kNarrowLong = 8192, kNarrowSteps = 8, kNarrowCount = 256, kMaxSlices = 16, kNarrowTiles = 6;
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
 struct NarrowGroup {
@@ -1141,6 +1355,9 @@ double product_cost(long long tiles, int tile, int planes, int k) {
   return rounds(256) * (8.0 + 1.64 * steps);
 }
 
+constexpr double kLaunch = 1.0;            // of a launch, us, beside its kernel's start
+constexpr int kMostPair = 256;              // the longest shorter side that pair_kernel holds in registers
+
 long long tiles_of(int mode, int mp, int np, int tile) {
   const long long m = mp / tile, n = np / tile;
   return mode == kGram || mode == kPoly ? m * (m + 1) / 2 : m * n;
@@ -1168,7 +1385,7 @@ int pick_tile(int mode, int planes, int pad, const Sizes& groups, int n, double*
 }
 
 struct Plan {
-  struct G { int planes, shorter, longer, pad, mp, np, count = 0, first = 0; size_t x[2], a, b, partial, q; float sigma; bool narrow; };   // matrices of one shape and type
+  struct G { int planes, shorter, longer, pad, mp, np, count = 0, first = 0; size_t x[2], a, b, partial, q; float sigma; bool narrow, pair = false; };   // matrices of one shape and type
   std::vector<G> groups;
   std::vector<int> group_of_tensor, first_of_tensor, parts;
   std::vector<size_t> u, partial;
@@ -1194,51 +1411,89 @@ void pad_to(Plan::G& g, int pad) {
   g.np = (g.longer + pad - 1) / pad * pad;
 }
 
-// A step of the groups of one type, those of one padding launched together; a launch costs some 4 us.
+// What share_gram_kernel and pair_kernel take for a step of the groups, in us, from their times over 1 to 24 matrices of 64 x 300 to 256 x 4000.  The strips' part grows
+// with the cube of the shorter side: its square in operands and products, and fewer workgroups at a time on a CU for the registers that hold A.  24 matrices
+// of 128 x 4000 in bfloat16: strips 14 us, where the second and third product take 18; one of 256 x 784 in float32 8 against 9, 16 of them 24 against 20.
+int share_tile(long long tiles_of_16) { return tiles_of_16 <= 512 ? 16 : 32; }   // tiles of 16 as long as a CU has two at most: 4 of 128 x 4000 in float32 7.4 us, of 32 13
+double pair_cost(const std::vector<Plan::G>& groups, int planes) {
+  long long tiles[2] = {0, 0};
+  int steps = 0;
+  double strips = 0.0;
+  for (const auto& g : groups) {
+    for (int h = 0; h < 2; ++h) tiles[h] += tiles_of(kGram, g.mp, g.np, 16 << h) * g.count;
+    steps = std::max(steps, g.np / 64);
+    strips += (double)(g.np / kStrip) * g.count / 256.0 * (0.3 + (planes == 2 ? 0.010 : 0.004) * std::pow(g.mp / 32.0, 3.0));
+  }
+  const int tile = share_tile(tiles[0]);
+  const double piece = (planes == 2 ? 0.06 : 0.03) * (tile == 16 ? 1.0 : 2.7);
+  return 3.0 + piece * steps * std::ceil(tiles[tile == 32] / 256.0) + 3.0 + strips + 2 * kLaunch;
+}
+
+// A step of the groups of one type, those of one padding launched together, and those of two launches a step.
 double step_cost(const std::vector<Plan::G>& groups, int planes) {
   double sum = 0.0;
-  for (int pad = 64; pad <= largest_tile(planes); pad *= 2) {
-    std::vector<Plan::G> some;
+  std::vector<Plan::G> some;
+  auto select = [&](auto&& which) {
+    some.clear();
     for (const auto& g : groups)
-      if (g.planes == planes && g.pad == pad && !g.narrow) some.push_back(g);
-    if (some.empty()) continue;
+      if (g.planes == planes && !g.narrow && which(g)) some.push_back(g);
+    return !some.empty();
+  };
+  if (select([](const Plan::G& g) { return g.pair; })) sum += pair_cost(some, planes);
+  for (int pad = 64; pad <= largest_tile(planes); pad *= 2) {
+    if (!select([&](const Plan::G& g) { return !g.pair && g.pad == pad; })) continue;
     for (int mode : {kGram, kPoly, kUpdate}) {
       double cost;
       pick_tile(mode, planes, pad, some, (int)some.size(), &cost);
-      sum += cost + 4.0;
+      sum += cost + kLaunch;
     }
   }
   return sum;
 }
 
-// Sides padded to multiples of 64, 128 or 256, which is what lets a product use tiles of that size: each group as is cheapest for it alone, or
-// all alike, whichever makes the step cheaper.
+// Sides padded to multiples of 64, 128 or 256, which is what lets a product use tiles of that size, and steps of two or three launches: each group as is
+// cheapest for it alone, or the paddings all alike, or no group in two launches, whichever makes the step cheapest.
 void choose_padding(std::vector<Plan::G>& groups, int planes) {
-  std::vector<Plan::G> best;
+  std::vector<Plan::G> best, own = groups;
   double least = 0.0;
-  auto consider = [&](std::vector<Plan::G> now) {
+  auto consider = [&](const std::vector<Plan::G>& now) {
     const double cost = step_cost(now, planes);
-    if (best.empty() || cost < least) { best = std::move(now); least = cost; }
+    if (best.empty() || cost < least) { best = now; least = cost; }
   };
-  std::vector<Plan::G> own = groups;
-  for (auto& g : own) {
+  std::vector<char> pair(groups.size(), 0);
+  for (size_t i = 0; i < own.size(); ++i) {
+    Plan::G& g = own[i];
     if (g.planes != planes) continue;
     double cheapest = 0.0;
     Plan::G pick = g;
-    for (int pad = 64; pad <= largest_tile(planes); pad *= 2) {
-      Plan::G q = g;
+    auto alone = [&](Plan::G q, int pad) {
       pad_to(q, pad);
+      q.narrow = false;   // (a narrow one of many steps)
       const double cost = step_cost({q}, planes);
-      if (pad == 64 || cost < cheapest) { pick = q; cheapest = cost; }
-    }
+      if (cheapest == 0.0 || cost < cheapest) { pick.pair = q.pair; if (!q.pair) pad_to(pick, pad); cheapest = cost; }
+    };
+    for (int pad = 64; pad <= largest_tile(planes); pad *= 2) alone(g, pad);
+    Plan::G two = g;
+    pad_to(two, 64);
+    two.pair = two.mp <= kMostPair;
+    if (two.pair) alone(two, 64);
+    pair[i] = pick.pair;
+    pick.pair = false;
     g = pick;
   }
-  consider(own);
-  for (int pad = 64; pad <= largest_tile(planes); pad *= 2) {
-    std::vector<Plan::G> alike = groups;
-    for (auto& g : alike)
-      if (g.planes == planes) pad_to(g, pad);
-    consider(alike);
+  for (int two = 0; two < 2; ++two) {
+    auto with_pairs = [&](std::vector<Plan::G> now) {
+      for (size_t i = 0; i < now.size(); ++i)
+        if (two && now[i].planes == planes && pair[i]) { now[i].pair = true; pad_to(now[i], 64); }
+      consider(now);
+    };
+    with_pairs(own);
+    for (int pad = 64; pad <= largest_tile(planes); pad *= 2) {
+      std::vector<Plan::G> alike = groups;
+      for (auto& g : alike)
+        if (g.planes == planes) pad_to(g, pad);
+      with_pairs(alike);
+    }
   }
   groups = std::move(best);
 }
@@ -1266,7 +1521,7 @@ Plan make_plan(const MuonTensor* t, int n) {
   }
   int first = 0;
   for (auto& g : p.groups) { g.first = first; first += g.count; }
-  for (auto& g : p.groups) g.narrow = g.shorter <= kNarrow && g.longer <= kNarrowLong && g.count <= kNarrowCount;
+  for (auto& g : p.groups) g.narrow = g.shorter <= narrow_side(g.planes) && g.longer <= kNarrowLong && g.count <= kNarrowCount;
   for (int planes = 1; planes <= 2; ++planes) choose_padding(p.groups, planes);
   p.matrices = take(sizeof(Matrix) * (size_t)p.n_matrices);
   for (int i = 0; i < n; ++i) {
@@ -1280,7 +1535,7 @@ Plan make_plan(const MuonTensor* t, int n) {
   }
   for (auto& g : p.groups) {
     const size_t x = (size_t)g.count * g.planes * g.mp * g.np * 2, a = (size_t)g.count * g.planes * g.mp * g.mp * 2;
-    g.x[0] = take(x); g.x[1] = take(x); g.a = take(a); g.b = take(a);
+    g.x[0] = take(x); g.x[1] = take(x); g.a = take(a); g.b = take(g.pair ? 0 : a);
     if (g.narrow) {   // (many steps take the other way)
       g.partial = take((size_t)g.count * kMaxSlices * narrow_tiles(g.shorter) * 256 * sizeof(double));
       g.q = take((size_t)g.count * ((size_t)g.shorter * g.shorter + 1) * sizeof(float));
@@ -1345,6 +1600,35 @@ hipError_t product(Groups& t, int pad, hipStream_t s) {
   }
 }
 
+template <bool FINAL, int PLANES>
+hipError_t launch_pair(Groups& t, hipStream_t s) {
+  int most = 0;
+  for (int i = 0; i < t.n; ++i) most = std::max(most, t.g[i].mp);
+  const int blocks = lay_out(t, [](const Group& g) { return g.np / kStrip; });
+  if (blocks < 0) return hipErrorInvalidValue;
+  auto go = [&](auto size) {
+    constexpr int MOST = decltype(size)::value;
+    hipLaunchKernelGGL((pair_kernel<FINAL, PLANES, MOST>), dim3((unsigned)blocks), dim3(2 * MOST), 0, s, t);
+    return hipGetLastError();
+  };
+  if (most <= 64) return go(std::integral_constant<int, 64>{});
+  if (most <= 128) return go(std::integral_constant<int, 128>{});
+  return go(std::integral_constant<int, 256>{});
+}
+template <int PLANES>
+hipError_t launch_share_gram(Groups& t, hipStream_t s) {
+  auto tiles = [&](int tile) { return lay_out(t, [&](const Group& g) { return tiles_of(kGram, g.mp, g.np, tile); }); };
+  int blocks = tiles(16);
+  if (blocks >= 0 && share_tile(blocks) == 16) {
+    hipLaunchKernelGGL((share_gram_kernel<PLANES, 16, PLANES == 2 ? 3 : 4>), dim3((unsigned)blocks), dim3(kShareThreads), 0, s, t);
+    return hipGetLastError();
+  }
+  blocks = tiles(32);
+  if (blocks < 0) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((share_gram_kernel<PLANES, 32, PLANES == 2 ? 2 : 3>), dim3((unsigned)blocks), dim3(kShareThreads), 0, s, t);
+  return hipGetLastError();
+}
+
 hipError_t narrow_steps(NarrowGroups t, int steps, hipStream_t s) {
   size_t chain_lds = 0;
   auto lay_out = [&](auto per_matrix) {
@@ -1369,20 +1653,25 @@ hipError_t narrow_steps(NarrowGroups t, int steps, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int PLANES>
+template <int PLANES, bool PAIR>
 hipError_t orthogonalise(Groups t, int pad, int steps, hipStream_t s) {
   int blocks = lay_out(t, [](const Group& g) { return (long long)(g.mp / 64) * (g.np / 64); });
   if (blocks < 0) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(normalise_kernel<PLANES>, dim3((unsigned)blocks), dim3(kThreads), 0, s, t);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  for (int k = 0; k < steps; ++k) {
-    if (hipError_t e = product<kGram, PLANES>(t, pad, s); e != hipSuccess) return e;
-    if (hipError_t e = product<kPoly, PLANES>(t, pad, s); e != hipSuccess) return e;
-    const hipError_t e = k + 1 < steps ? product<kUpdate, PLANES>(t, pad, s) : product<kFinal, PLANES>(t, pad, s);
-    if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((normalise_kernel<PLANES, PAIR>), dim3((unsigned)blocks), dim3(kThreads), 0, s, t);
+  hipError_t e = hipGetLastError();
+  for (int k = 0; k < steps && e == hipSuccess; ++k) {
+    const bool last = k + 1 == steps;
+    if constexpr (PAIR) {
+      e = launch_share_gram<PLANES>(t, s);
+      if (e == hipSuccess) e = last ? launch_pair<true, PLANES>(t, s) : launch_pair<false, PLANES>(t, s);
+    } else {
+      e = product<kGram, PLANES>(t, pad, s);
+      if (e == hipSuccess) e = product<kPoly, PLANES>(t, pad, s);
+      if (e == hipSuccess) e = last ? product<kFinal, PLANES>(t, pad, s) : product<kUpdate, PLANES>(t, pad, s);
+    }
     for (int i = 0; i < t.n; ++i) std::swap(t.g[i].x[0], t.g[i].x[1]);
   }
-  return hipSuccess;
+  return e;
 }
 
 }  // namespace
@@ -1443,25 +1732,31 @@ hipError_t launch_muon_step(const MuonTensor* tensors, int n, const spb_muon_con
     if (t.n == 0) break;
     if (hipError_t e = narrow_steps(t, c.ns_steps, stream); e != hipSuccess) return e;
   }
-  for (int planes = 1; planes <= 2; ++planes)
-    for (int pad = 64; pad <= largest_tile(planes); pad *= 2) {
-      size_t k = 0;
-      while (k < p.groups.size()) {
-        Groups t = {};
-        for (; k < p.groups.size() && t.n < kMaxGroups; ++k) {
-          const Plan::G& s = p.groups[k];
-          if (s.planes != planes || s.pad != pad || (s.narrow && few_steps)) continue;
-          Group& d = t.g[t.n++];
-          d.x[0] = reinterpret_cast<_Float16*>(ws + s.x[0]); d.x[1] = reinterpret_cast<_Float16*>(ws + s.x[1]);
-          d.a = reinterpret_cast<_Float16*>(ws + s.a); d.b = reinterpret_cast<_Float16*>(ws + s.b);
-          d.matrices = matrices + s.first;
-          d.mp = s.mp; d.np = s.np; d.count = s.count; d.sigma = s.sigma;
-        }
-        if (t.n == 0) break;
-        const hipError_t e = planes == 1 ? orthogonalise<1>(t, pad, c.ns_steps, stream) : orthogonalise<2>(t, pad, c.ns_steps, stream);
-        if (e != hipSuccess) return e;
+  // pad 0: the groups of two launches a step
+  auto steps_of = [&](int planes, int pad) {
+    for (size_t k = 0; k < p.groups.size();) {
+      Groups t = {};
+      for (; k < p.groups.size() && t.n < kMaxGroups; ++k) {
+        const Plan::G& s = p.groups[k];
+        if (s.planes != planes || (s.pair ? 0 : s.pad) != pad || (s.narrow && few_steps)) continue;
+        Group& d = t.g[t.n++];
+        d.x[0] = reinterpret_cast<_Float16*>(ws + s.x[0]); d.x[1] = reinterpret_cast<_Float16*>(ws + s.x[1]);
+        d.a = reinterpret_cast<_Float16*>(ws + s.a); d.b = reinterpret_cast<_Float16*>(ws + s.b);
+        d.matrices = matrices + s.first;
+        d.mp = s.mp; d.np = s.np; d.count = s.count; d.sigma = s.sigma;
       }
+      if (t.n == 0) break;
+      const hipError_t e = pad == 0 ? planes == 1 ? orthogonalise<1, true>(t, pad, c.ns_steps, stream) : orthogonalise<2, true>(t, pad, c.ns_steps, stream)
+                                    : planes == 1 ? orthogonalise<1, false>(t, pad, c.ns_steps, stream) : orthogonalise<2, false>(t, pad, c.ns_steps, stream);
+      if (e != hipSuccess) return e;
     }
+    return hipSuccess;
+  };
+  for (int planes = 1; planes <= 2; ++planes) {
+    if (hipError_t e = steps_of(planes, 0); e != hipSuccess) return e;
+    for (int pad = 64; pad <= largest_tile(planes); pad *= 2)
+      if (hipError_t e = steps_of(planes, pad); e != hipSuccess) return e;
+  }
   return hipSuccess;
 }
 

@@ -4,8 +4,9 @@ Tolerances, with u = 2^-24.  Moments: two roundings an addition, (contributors +
 step of the storage type.  The orthogonalised matrix, in the Frobenius norm: the Newton-Schulz step's divided differences (p(s) - p(t)) / (s - t) and
 (p(s) + p(t)) / (s + t) are at most L = 3.4445 in magnitude where singular values stay below 1.3, so an error grows at most L-fold a step; a step adds the
 rounding of X, A and B to h relative (h = 2^-11 for bfloat16 parameters, 2^-21 for float32 ones: value and remainder, each product's remainder x remainder
-left out) and that of its three sums (k / 16 + 16) u of |P| |Q| each.  `bound` adds these up along the exact iterates.  Applied to w = 0, what is left is the
-storage type's half step."""
+left out) and that of its three sums (k / 16 + 16) u of |P| |Q| each.  A step of two launches rounds Z = b X + c A X in the place of B, and multiplies it by A:
+h |Z| |A| where the other has h |B| |X|, of which `bound` takes the larger; its sums b X + A (c X) and A Z stay below those of B and B X.  `bound` adds these up along
+the exact iterates.  Applied to w = 0, what is left is the storage type's half step."""
 import ctypes as C
 import math
 
@@ -37,8 +38,9 @@ def bound(u, dtype, hyper):
         b = -4.7750 * a + 2.0315 * a @ a
         new = GROWTH * x + b @ x
         off_a = h * fro(a) + chain(x.shape[1]) * fro(x) ** 2
-        off_b = h * fro(b) + (4.7750 + 2 * 2.0315 * two(a)) * off_a + 2.0315 * chain(len(a)) * fro(a) ** 2
-        err = GROWTH * err + off_b * two(x) + chain(len(a)) * fro(b) * fro(x) + (h + 4 * U) * fro(new)
+        off_b = (4.7750 + 2 * 2.0315 * two(a)) * off_a + 2.0315 * chain(len(a)) * fro(a) ** 2
+        stored = h * max(fro(b) * two(x), two(a) * fro(-4.7750 * x + 2.0315 * a @ x))
+        err = GROWTH * err + stored + off_b * two(x) + chain(len(a)) * fro(b) * fro(x) + (h + 4 * U) * fro(new)
         x = new
     return err
 
@@ -113,7 +115,13 @@ MATRICES = {
     "square": dict(shape=(384, 384), blocks=1, workers=2, rank=8),
     "stem": dict(shape=(64, 7, 7, 3), blocks=1, workers=2),
     "conv": dict(shape=(96, 3, 3, 24), blocks=1, workers=1),
+    "narrow_33_wide": dict(shape=(33, 8192), blocks=1, workers=1, rank=2),
     "vector": dict(shape=(150,), blocks=1, workers=1),
+    "stack_64": dict(shape=(70 * 60, 90), blocks=70, workers=1),
+    "stack_192": dict(shape=(3, 190, 300), blocks=3, workers=2, rank=2),
+    "stack_128": dict(shape=(24, 140, 120), blocks=24, workers=1),
+    "stack_256": dict(shape=(16, 250, 600), blocks=16, workers=1, rank=2),
+    "long_64": dict(shape=(2, 5000, 57), blocks=2, workers=1, rank=1),
     "narrow_16": dict(shape=(16, 1000), blocks=1, workers=2, rank=3),
     "narrow_33": dict(shape=(5 * 33, 130), blocks=5, workers=1),
     "narrow_48_long": dict(shape=(48, 8192), blocks=1, workers=1, rank=2),
@@ -187,7 +195,7 @@ def test_every_entry_of_a_float32_matrix(shape, steps):
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("shape", [(48, 150), (150, 33), (17, 17), (1, 9)])
 def test_a_short_side_in_one_and_in_many_products(shape, dtype):
-    """Up to 8 steps run on the small Gram matrix, more as products of the whole: both against the formula, whose 8 and 9 steps differ."""
+    """Up to 8 steps may run on the small Gram matrix, more as products of the whole: both against the formula, whose 8 and 9 steps differ."""
     for steps in (1, 2, 3, 8, 9, 16):
         hyper = {**HYPER, "ns_steps": steps}
         t = _tensor(shape, 1, dtype, 2, seed=12, w=0.0)
