@@ -35,6 +35,10 @@ using gemm_dma_detail::wait_loads_and_barrier;
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+// the same as they lie at any element's address: one access all the same (gfx950 takes global addresses of any alignment)
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4_t;
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
@@ -48,7 +52,7 @@ struct Matrix {
   void* w;                 // first element of the matrix in its parameter
   const float* u;          // [rows, cols] dense
   const double* partial;   // [parts] sums of u^2
-  int parts, rows, cols, bf16, vector;   // vector: 8 entries of a row are whole 16-byte pieces
+  int parts, rows, cols, bf16;
   float keep, step, eps;   // w = keep * w - step * X
 };
 
@@ -67,7 +71,7 @@ struct Tensor {
   long long numel;         // of one block
   long long chunk;         // elements of one workgroup
   int blocks, parts;       // matrices, workgroups of each
-  int first_block, count, bf16, rows, cols, vector;
+  int first_block, count, bf16, rows, cols;
   float rate, keep, step;   // keep = 1 - rate * weight decay
 };
 struct Table {
@@ -95,13 +99,13 @@ template <int C, bool MATRIX>
 __device__ __forceinline__ void step_vector(const Table& tab, const Tensor& t, long long e0, float inv, double& sq) {
   f32x4 x[C], v = {}, w = {};
 #pragma unroll
-  for (int j = 0; j < C; ++j) x[j] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(t.g[j] + e0));   // read once
-  f32x4 m = *reinterpret_cast<const f32x4*>(t.m + e0);
-  uint2 wb = {};
+  for (int j = 0; j < C; ++j) x[j] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any*>(t.g[j] + e0));   // read once
+  f32x4 m = *reinterpret_cast<const f32x4_any*>(t.m + e0);
+  u32x2_any wb = {};
   if constexpr (!MATRIX) {
-    v = *reinterpret_cast<const f32x4*>(t.v + e0);
-    if (t.bf16) wb = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(t.w) + e0);
-    else w = *reinterpret_cast<const f32x4*>(static_cast<const float*>(t.w) + e0);
+    v = *reinterpret_cast<const f32x4_any*>(t.v + e0);
+    if (t.bf16) wb = *reinterpret_cast<const u32x2_any*>(static_cast<const uint16_t*>(t.w) + e0);
+    else w = *reinterpret_cast<const f32x4_any*>(static_cast<const float*>(t.w) + e0);
   }
   f32x4 g = {0.f, 0.f, 0.f, 0.f}, u = {};
 #pragma unroll
@@ -113,23 +117,22 @@ __device__ __forceinline__ void step_vector(const Table& tab, const Tensor& t, l
     step_element<MATRIX>(tab, t, g[e] * inv, me, ve, we, ue);
     m[e] = me; v[e] = ve; w[e] = we; u[e] = ue;
   }
-  *reinterpret_cast<f32x4*>(t.m + e0) = m;
+  *reinterpret_cast<f32x4_any*>(t.m + e0) = m;
   if constexpr (MATRIX) {
-    *reinterpret_cast<f32x4*>(t.u + e0) = u;
+    *reinterpret_cast<f32x4_any*>(t.u + e0) = u;
 #pragma unroll
     for (int e = 0; e < 4; ++e) sq += (double)u[e] * (double)u[e];
   } else {
-    *reinterpret_cast<f32x4*>(t.v + e0) = v;
-    if (t.bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(t.w) + e0) = uint2{bf16_pack2(w[0], w[1]), bf16_pack2(w[2], w[3])};
-    else *reinterpret_cast<f32x4*>(static_cast<float*>(t.w) + e0) = w;
+    *reinterpret_cast<f32x4_any*>(t.v + e0) = v;
+    if (t.bf16) *reinterpret_cast<u32x2_any*>(static_cast<uint16_t*>(t.w) + e0) = u32x2_any{bf16_pack2(w[0], w[1]), bf16_pack2(w[2], w[3])};
+    else *reinterpret_cast<f32x4_any*>(static_cast<float*>(t.w) + e0) = w;
   }
 }
-// The same element by element: any number of elements, any alignment.
+// The same element by element: the last three at most.  (Element by element throughout, 11.9 million float32 of six workers took 352 us, where four at a time take
+// 94.)
 template <bool MATRIX>
 __device__ __forceinline__ void step_scalar(const Table& tab, const Tensor& t, long long e0, long long end, float inv, double& sq) {
-  const int live = (int)min(end - e0, 4ll);
-  for (int e = 0; e < live; ++e) {
-    const long long at = e0 + e;
+  for (long long at = e0; at < end; ++at) {
     float g = 0.f, m = t.m[at], v = 0.f, w = 0.f, u = 0.f;
     for (int j = 0; j < t.count; ++j) g += t.g[j][at];
     if (!MATRIX) {
@@ -152,13 +155,13 @@ template <int C, bool MATRIX>
 __device__ __forceinline__ void step_range(const Table& tab, const Tensor& t, long long begin, long long end, double& sq) {
   const float inv = 1.f / (float)t.count;
   for (long long e0 = begin + threadIdx.x * 4; e0 < end; e0 += kThreads * 4) {
-    if constexpr (C > 0) step_vector<C, MATRIX>(tab, t, e0, inv, sq);
+    if (e0 + 4 <= end) step_vector<C, MATRIX>(tab, t, e0, inv, sq);
     else step_scalar<MATRIX>(tab, t, e0, end, inv, sq);
   }
 }
 template <bool MATRIX>
 __device__ __forceinline__ void step_tensor(const Table& tab, const Tensor& t, long long begin, long long end, double& sq) {
-  switch (t.vector ? t.count : 0) {   // uniform over the workgroup
+  switch (t.count) {   // uniform over the workgroup
     case 1: step_range<1, MATRIX>(tab, t, begin, end, sq); return;
     case 2: step_range<2, MATRIX>(tab, t, begin, end, sq); return;
     case 3: step_range<3, MATRIX>(tab, t, begin, end, sq); return;
@@ -166,8 +169,7 @@ __device__ __forceinline__ void step_tensor(const Table& tab, const Tensor& t, l
     case 5: step_range<5, MATRIX>(tab, t, begin, end, sq); return;
     case 6: step_range<6, MATRIX>(tab, t, begin, end, sq); return;
     case 7: step_range<7, MATRIX>(tab, t, begin, end, sq); return;
-    case 8: step_range<8, MATRIX>(tab, t, begin, end, sq); return;
-    default: step_range<0, MATRIX>(tab, t, begin, end, sq);
+    default: step_range<kMaxAggWorkers, MATRIX>(tab, t, begin, end, sq);
   }
 }
 
@@ -193,7 +195,7 @@ __global__ __launch_bounds__(kThreads) void update_kernel(Table tab) {
     t.partial[(long long)mat * t.parts + part] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     if (part == 0)
       t.out[mat] = Matrix{t.bf16 ? (void*)(static_cast<uint16_t*>(t.w) + base) : (void*)(static_cast<float*>(t.w) + base), t.u + base,
-                          t.partial + (long long)mat * t.parts, t.parts, t.rows, t.cols, t.bf16, t.vector && t.cols % 8 == 0, t.keep, t.step, tab.ns_eps};
+                          t.partial + (long long)mat * t.parts, t.parts, t.rows, t.cols, t.bf16, t.keep, t.step, tab.ns_eps};
   }
 }
 
@@ -301,7 +303,7 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(Groups groups) {
     const float* src = d.u + (size_t)(r0 + r) * d.cols + c0 + c;
     in[k] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (r0 + r >= d.rows) continue;
-    if (c0 + c + 4 <= d.cols && (d.cols & 3) == 0) in[k] = *reinterpret_cast<const f32x4*>(src);
+    if (c0 + c + 4 <= d.cols) in[k] = *reinterpret_cast<const f32x4_any*>(src);
     else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -328,13 +330,13 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(Groups groups) {
 // 8 entries of one row of the parameter (bfloat16 with one plane, float32 with two) as they are before the step, requested ahead where they are whole
 // 16-byte pieces.
 template <int PLANES> struct Entries { u32x4 c[PLANES]; };
-__device__ __forceinline__ bool whole8(const Matrix& d, int row, int col) { return d.vector && row < d.rows && col + 8 <= d.cols; }
+__device__ __forceinline__ bool whole8(const Matrix& d, int row, int col) { return row < d.rows && col + 8 <= d.cols; }
 template <int PLANES>
 __device__ __forceinline__ void request8(const Matrix& d, int row, int col, Entries<PLANES>& to) {
   if (!whole8(d, row, col)) return;
   const char* w = static_cast<const char*>(d.w) + ((size_t)row * d.cols + col) * (PLANES == 2 ? 4 : 2);
 #pragma unroll
-  for (int h = 0; h < PLANES; ++h) to.c[h] = *reinterpret_cast<const u32x4*>(w + 16 * h);
+  for (int h = 0; h < PLANES; ++h) to.c[h] = *reinterpret_cast<const u32x4_any*>(w + 16 * h);
 }
 // w = keep * w - step * X; v: sigma X.
 template <int PLANES>
@@ -349,7 +351,7 @@ __device__ __forceinline__ void apply8(const Matrix& d, float inv_sigma, const f
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         out[e] = bf16_pack2(d.keep * __uint_as_float(old.c[0][e] << 16) - step * v[2 * e], d.keep * __uint_as_float(old.c[0][e] & 0xFFFF0000u) - step * v[2 * e + 1]);
-      *reinterpret_cast<u32x4*>(w) = out;
+      *reinterpret_cast<u32x4_any*>(w) = out;
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -363,7 +365,7 @@ __device__ __forceinline__ void apply8(const Matrix& d, float inv_sigma, const f
         f32x4 out;
 #pragma unroll
         for (int e = 0; e < 4; ++e) out[e] = d.keep * __uint_as_float(old.c[h][e]) - step * v[4 * h + e];
-        *reinterpret_cast<f32x4*>(w + 4 * h) = out;
+        *reinterpret_cast<f32x4_any*>(w + 4 * h) = out;
       }
     } else {
 #pragma unroll
@@ -1703,9 +1705,7 @@ hipError_t launch_muon_step(const MuonTensor* tensors, int n, const spb_muon_con
       d.numel = numel; d.parts = (int)parts; d.chunk = chunk;
       d.rows = (int)(matrix ? s.rows / s.blocks : 0); d.cols = (int)(matrix ? s.cols : 0);
       d.first_block = (int)blocks;
-      uintptr_t bits = (uintptr_t)s.w | (uintptr_t)s.m | (uintptr_t)s.v;
-      for (int j = 0; j < s.count; ++j) { d.g[j] = s.g[j]; bits |= (uintptr_t)s.g[j]; }
-      d.vector = (bits & 15) == 0 && d.numel % 4 == 0;
+      for (int j = 0; j < s.count; ++j) d.g[j] = s.g[j];
       if (matrix) {
         d.u = reinterpret_cast<float*>(ws + p.u[i]);
         d.partial = reinterpret_cast<double*>(ws + p.partial[i]);
