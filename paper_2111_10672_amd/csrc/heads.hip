@@ -83,22 +83,51 @@ struct Args {
   double turns[SPB_MAX_PAIRS];     // turns per unit of position
 };
 
-struct Token { long long x, g, o; };
+struct Token { long long x, g, o, pos; };
+
+// Which token of a block and which of `heads` heads (or pairs) row r is: r < 2^20, so float32 divides it exactly.
+__device__ __forceinline__ void place_of(int r, int heads, float inv_heads, int& token, int& head) {
+  token = (int)(((float)r + 0.5f) * inv_heads);
+  head = r - token * heads;
+}
+
+// Cosine and sine of `turn` turns, |turn| <= 1/2: the nearest quarter aside, the series at most an eighth of a turn from zero, up to the ninth and the
+// tenth power, whose remainders are below 2^-29.
+__device__ __forceinline__ float2 cos_sin(float turn) {
+  constexpr double T = 2.0 * M_PI, T2 = T * T;
+  const float quarter = rintf(4.f * turn), y = fmaf(quarter, -0.25f, turn), z = y * y;   // (y is exact)
+  float s = (float)(T * T2 * T2 * T2 * T2 / 362880.0);
+  s = fmaf(s, z, (float)(-T * T2 * T2 * T2 / 5040.0));
+  s = fmaf(s, z, (float)(T * T2 * T2 / 120.0));
+  s = fmaf(s, z, (float)(-T * T2 / 6.0));
+  s = fmaf(s, z, (float)T) * y;
+  float c = (float)(-T2 * T2 * T2 * T2 * T2 / 3628800.0);
+  c = fmaf(c, z, (float)(T2 * T2 * T2 * T2 / 40320.0));
+  c = fmaf(c, z, (float)(-T2 * T2 * T2 / 720.0));
+  c = fmaf(c, z, (float)(T2 * T2 / 24.0));
+  c = fmaf(c, z, (float)(-T2 / 2.0));
+  c = fmaf(c, z, 1.f);
+  const int q = (int)quarter;
+  const float cn = q & 1 ? s : c, sn = q & 1 ? c : s;
+  return make_float2((q + 1) & 2 ? -cn : cn, q & 2 ? -sn : sn);
+}
 
 // Offsets of the tokens of a block and the cosines and sines of their pairs, into LDS.
 __device__ __forceinline__ void load_tokens(const Args& a, unsigned first, int n, Token* tok, float2* cs) {
   if ((int)threadIdx.x < n) {
     const unsigned t = first + threadIdx.x, b = t / (unsigned)a.seq, s = t - b * a.seq;
-    tok[threadIdx.x] = Token{(long long)b * a.xs[0] + (long long)s * a.xs[1], (long long)b * a.gs[0] + (long long)s * a.gs[1], (long long)b * a.os[0] + (long long)s * a.os[1]};
+    tok[threadIdx.x] = Token{(long long)b * a.xs[0] + (long long)s * a.xs[1], (long long)b * a.gs[0] + (long long)s * a.gs[1],
+                             (long long)b * a.os[0] + (long long)s * a.os[1], (long long)b * a.pos_batch + s};
   }
+  __syncthreads();
+  const float inv_pairs = 1.f / (float)a.pairs;
   for (int i = threadIdx.x; i < n * a.pairs; i += kThreads) {
-    const int k = i / a.pairs, j = i - k * a.pairs;
-    const unsigned t = first + k, b = t / (unsigned)a.seq, s = t - b * a.seq;
-    double turn = (double)a.pos[a.axis[j] * a.pos_axis + (long long)b * a.pos_batch + s] * a.turns[j];
+    int k, j;
+    place_of(i, a.pairs, inv_pairs, k, j);
+    double turn = (double)a.pos[a.axis[j] * a.pos_axis + tok[k].pos] * a.turns[j];
     turn -= rint(turn);
-    float sn, cn;
-    sincospif(2.f * (float)turn, &sn, &cn);
-    cs[i] = make_float2(cn, a.inverse ? -sn : sn);
+    const float2 t = cos_sin((float)turn);
+    cs[i] = make_float2(t.x, a.inverse ? -t.y : t.y);
   }
 }
 
@@ -167,12 +196,6 @@ __device__ __forceinline__ float centre(float (&u)[V], float (&v)[V], bool has0,
     sq += u[e] * u[e] + v[e] * v[e];
   }
   return 1.f / sqrtf(group_sum<G>(sq) * inv_dim + eps);
-}
-
-// Which token of a block and which of `heads` heads row r is: r < 2^20, so float32 divides it exactly.
-__device__ __forceinline__ void place_of(int r, int heads, float inv_heads, int& token, int& head) {
-  token = (int)(((float)r + 0.5f) * inv_heads);
-  head = r - token * heads;
 }
 
 // The two chunks of a row that a lane holds.
