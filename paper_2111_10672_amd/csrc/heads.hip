@@ -9,7 +9,7 @@
 // Memory-bound: every element is read once and written once, statistics are formed from the row in registers (the
 // backward pass forms them again rather than read them).  32792 tokens of 32 heads of 128 in bfloat16, normed and half of each head turned: 107 us, 5.0 TB/s;
 // backward, 16384 tokens of 24 + 8 heads of 128 normed and turned: 91 us and 4 us for the sums, 4.2 TB/s.  What threatens to bound it instead is the angles: cosine and
-// sine of a far position in enough bits take a few hundred instruction slots a pair.  So a workgroup takes all heads of a
+// sine of a far position in enough bits take some hundred instruction slots a pair.  So a workgroup takes all heads of a
 // few tokens and works the angles out once per token and pair, into LDS, where every head of the token reads them.
 //
 // An angle is formed as a fraction of a turn in float64: positions are whole numbers, so position times turns per unit, less
@@ -28,7 +28,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
-constexpr int kMaxTokensPerBlock = 16;
+constexpr int kMaxTokensPerBlock = 64, kMaxTurnedTokens = 16;
+constexpr int kMaxAnglesPerBlock = 2048;    // 16 KB of LDS
 
 struct bf16_t { uint16_t bits; };
 __device__ __forceinline__ float to_float(float v) { return v; }
@@ -581,9 +582,10 @@ Route route_of(const HeadsProblem& q, bool sums) {
     while (r.lanes * 2 * v < q.head_dim) r.lanes *= 2;
   }
   const int at_once = r.lanes ? kThreads / r.lanes : kThreads / 64;   // rows a workgroup works on at a time
+  const int most = sums || !q.pairs ? std::min(kMaxTokensPerBlock, kMaxAnglesPerBlock / std::max(q.pairs, 1)) : kMaxTurnedTokens;
   auto tokens_for = [&](int heads) {
     const long long want = ((long long)(sums ? 3 : 4) * at_once + heads - 1) / heads;
-    return (int)std::max<long long>(1, std::min<long long>({want, kMaxTokensPerBlock, tokens / (sums ? 256 : 1024)}));
+    return (int)std::max<long long>(1, std::min<long long>({want, most, tokens / (sums ? 256 : 1024)}));
   };
   r.tokens_per_block = tokens_for(sums ? q.heads_q : q.heads_q + q.heads_k);
   if (sums && q.heads_k) r.tokens_per_block_k = tokens_for(q.heads_k);
