@@ -270,19 +270,31 @@ static void sides_of(const spb::ParamInfo& p, long long* rows, long long* cols) 
   *cols = p.numel() / p.shape[0];
 }
 
+// shapes, types and blocks of the parameters of units from `unit` on, which is what the deepest worker of a step leaves to update
+static int suffix_of(const spb::Model& im, const int32_t* blocks, int unit, std::vector<spb::MuonTensor>* t, const char* who) {
+  for (size_t i = 0; i < im.params.size(); ++i) {
+    if (im.params[i].unit < unit) continue;
+    spb::MuonTensor d;
+    sides_of(im.params[i], &d.rows, &d.cols);
+    if (int rc = check_shape(d.rows, d.cols, blocks[i], im.params[i].name.c_str(), who)) return rc;
+    d.blocks = blocks[i]; d.dtype = im.params[i].dtype;
+    t->push_back(d);
+  }
+  return SPB_OK;
+}
+
 int spb_aggregate_muon_workspace_size(const spb_model* m, const int32_t* blocks, size_t* bytes) {
   const char* who = "spb_aggregate_muon_workspace_size";
   SPB_REQUIRE(m && blocks && bytes, SPB_ERR_INVALID_ARG, "%s: null argument", who);
   return guarded(who, [&] {
-    std::vector<spb::MuonTensor> t;
-    for (size_t i = 0; i < m->impl->params.size(); ++i) {
-      spb::MuonTensor d;
-      sides_of(m->impl->params[i], &d.rows, &d.cols);
-      if (int rc = check_shape(d.rows, d.cols, blocks[i], m->impl->params[i].name.c_str(), who)) return rc;
-      d.blocks = blocks[i]; d.dtype = m->impl->params[i].dtype;
-      t.push_back(d);
+    size_t most = 0;
+    // (fewer tensors may need more: how matrices are padded goes by what is launched with them)
+    for (int unit = 0; unit < m->impl->num_units; ++unit) {
+      std::vector<spb::MuonTensor> t;
+      if (int rc = suffix_of(*m->impl, blocks, unit, &t, who)) return rc;
+      most = std::max(most, spb::muon_workspace_size(t.data(), (int)t.size()));
     }
-    *bytes = spb::muon_workspace_size(t.data(), (int)t.size());
+    *bytes = most;
     return SPB_OK;
   });
 }
@@ -319,9 +331,7 @@ int spb_aggregate_muon(spb_model* m, int32_t n_workers, const int32_t* depths, v
       d.rate = scale_lr ? config->lr * d.count / n_workers : config->lr;
       t.push_back(d);
     }
-    size_t need = 0;
-    if (int rc = spb_aggregate_muon_workspace_size(m, blocks, &need)) return rc;
-    if (int rc = check_workspace(workspace, workspace_bytes, need, who)) return rc;
+    if (int rc = check_workspace(workspace, workspace_bytes, spb::muon_workspace_size(t.data(), (int)t.size()), who)) return rc;
     if (int rc = check_tensors(t, who)) return rc;
     return launched(spb::launch_muon_step(t.data(), (int)t.size(), *config, workspace, static_cast<hipStream_t>(stream)), who);
   });

@@ -442,3 +442,19 @@ def test_server_step_arguments():
         assert e.value.code == -1
     finally:
         spb.spb_model_destroy(m)
+
+@pytest.mark.parametrize("dtype,dims", [("bf16", [56, 64, 8, 1192, 8]), ("bf16", [64, 104, 24, 2400, 8, 48]), ("f32", [232, 160, 2712, 568, 8])])
+def test_the_server_steps_workspace_covers_every_depth(dtype, dims):
+    """Few tensors can need more than many: their matrices are padded for themselves."""
+    cfg = dict(family="mlp", dtype=dtype, batch=4, dims=dims)
+    m = spb.spb_model_create(spb.desc_from_config(cfg))
+    try:
+        infos = [spb.spb_param_info(m, i) for i in range(spb.spb_param_count(m))]
+        blocks = [int(len(p["shape"]) > 1) for p in infos]
+        size = spb.spb_aggregate_muon_workspace_size(m, blocks)
+        stored = torch.bfloat16 if dtype == "bf16" else torch.float32
+        for unit in range(len(dims) - 1):
+            some = [dict(w=torch.empty(p["shape"], dtype=stored), blocks=b) for p, b in zip(infos, blocks) if p["unit"] >= unit]
+            assert spb.spb_muon_workspace_size(some) <= size, unit
+    finally:
+        spb.spb_model_destroy(m)
