@@ -370,7 +370,7 @@ int spb_muon_workspace_size(const spb_muon_tensor* tensors, int32_t n, size_t* b
 
 /* One step over n tensors, enqueued on `stream`; needs no model, allocates nothing and may be captured into a HIP graph.
  *   workspace  device, 256-byte aligned, until the call has completed on the device; NULL if the size is 0
- * Errors: INVALID_ARG (null or misaligned pointers, the same w twice, values outside their ranges), WORKSPACE, HIP. */
+ * Errors: INVALID_ARG (null or misaligned pointers, the same w, m or v twice, values outside their ranges), WORKSPACE, HIP. */
 int spb_muon_step(const spb_muon_tensor* tensors, int32_t n, const spb_muon_config* config, void* workspace, size_t workspace_bytes, void* stream);
 
 /* spb_aggregate_update with the step above in place of SGD: same workers, depths, averaging and rate scaling.

@@ -117,9 +117,13 @@ int check_tensors(const std::vector<spb::MuonTensor>& t, const char* who) {
     if (x.blocks) padded += (__int128)x.blocks * ((x.rows / x.blocks + 255) / 256 * 256) * ((x.cols + 255) / 256 * 256);
   SPB_REQUIRE(padded <= kMostEntries, SPB_ERR_INVALID_ARG, "%s: too many matrices for one call", who);
   std::vector<const void*> seen;
-  for (const auto& x : t) seen.push_back(x.w);
+  for (const auto& x : t) {
+    seen.push_back(x.w);
+    seen.push_back(x.m);
+    if (x.v) seen.push_back(x.v);
+  }
   std::sort(seen.begin(), seen.end());
-  SPB_REQUIRE(std::adjacent_find(seen.begin(), seen.end()) == seen.end(), SPB_ERR_INVALID_ARG, "%s: the same parameter twice", who);
+  SPB_REQUIRE(std::adjacent_find(seen.begin(), seen.end()) == seen.end(), SPB_ERR_INVALID_ARG, "%s: the same parameter or moment twice", who);
   return SPB_OK;
 }
 

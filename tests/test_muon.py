@@ -382,7 +382,7 @@ def test_tensors_and_settings_that_are_refused():
 
     for patch in (dict(rows=0), dict(cols=0), dict(rows=1 << 31), dict(rows=1 << 62), dict(rows=131073 * 4, blocks=131073, n=1), dict(blocks=-1), dict(blocks=4), dict(rows=65537, blocks=1), dict(cols=65537), dict(dtype=2), dict(count=0), dict(count=9),
                   dict(grads=None), dict(w=0), dict(w=1025), dict(m=0), dict(m=258), dict(v=0, blocks=0), dict(v=257, blocks=0), dict(rate_scale=-1.0), dict(rate_scale=float("nan")),
-                  dict(n=-1), dict(n=2, twice=True)):
+                  dict(n=-1), dict(n=2, twice=True), dict(n=2), dict(blocks=0)):      # (m and v are at one address)
         with pytest.raises(spb.SpbError) as e:
             call(**patch)
         assert e.value.code == -1, patch
