@@ -8,8 +8,10 @@
 //   others     m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2;  w = w (1 - rate wd) - rate (m / c1) / (sqrt(v / c2) + eps)
 //
 // The elementwise half is memory-bound and one launch over a table of tensors (update_kernel); for matrices it leaves u
-// (float32) and the partial sums of |u|^2 (float64, so that neither tiny nor huge gradients leave the range) in the workspace.
-// The products are bound by the matrix cores.  All matrices of one padded shape go through a product in one launch, whichever
+// (float32) and the partial sums of |u|^2 (float64, so that neither tiny nor huge gradients leave the range) in the workspace.  24 matrices of
+// 4096 x 1024 with one worker: 279 us, 5.8 TB/s; AdamW of 23.4 million bfloat16 with four: 146 us, 5.8 TB/s.
+// The products are bound by the matrix cores where there are many tiles (24 of 1024 x 4096 x 1024: 207 us, 1.0 PFLOP/s), by launches and latency where there
+// are few; kernels for each are below.  All matrices of one padding go through a product in one launch, whichever
 // tensors and blocks they come from, and the two symmetric products form the tiles on and below the diagonal only and
 // write each twice: a step of an r x c matrix costs r^2 c + r^3 + 2 r^2 c operations instead of 2 r^2 c + 2 r^3 + 2 r^2 c.
 //
