@@ -119,8 +119,8 @@ EXPORTS = {
     "spb_heads_backward": (C.c_int, [C.POINTER(spb_heads_desc), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p,
                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "spb_encoder_heads": (C.c_int, [C.c_void_p, C.POINTER(spb_rotary), C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_float]),
-    "spb_muon_workspace_size": (C.c_int, [C.POINTER(spb_muon_tensor), C.c_int32, C.POINTER(C.c_size_t)]),
-    "spb_muon_step": (C.c_int, [C.POINTER(spb_muon_tensor), C.c_int32, C.POINTER(spb_muon_config), C.c_void_p, C.c_size_t, C.c_void_p]),
+    "spb_muon_workspace_size": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(C.c_size_t)]),
+    "spb_muon_step": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(spb_muon_config), C.c_void_p, C.c_size_t, C.c_void_p]),
     "spb_aggregate_muon_workspace_size": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_size_t)]),
     "spb_aggregate_muon": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_void_p), C.POINTER(C.c_int32), C.POINTER(C.c_void_p),
                                      C.POINTER(C.c_void_p), C.POINTER(spb_muon_config), C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
@@ -424,45 +424,48 @@ def muon_config(lr, rms=0.2, momentum=0.95, nesterov=True, ns_steps=5, ns_eps=1e
 
 _MUON = struct.Struct("<4Q2qd4i")      # spb_muon_tensor
 assert _MUON.size == C.sizeof(spb_muon_tensor)
+_MUON_LAYOUT = "m, v and gradients are contiguous float32 tensors of the parameter's shape, which is contiguous too"
+_F32 = DTYPES["f32"]
 
 
 def _muon_tensors(tensors, pointers=True):
-    """ctypes list of tensors given as dict(w, m, v=None, grads=[...], blocks=0, rate_scale=1.0), and what keeps its arrays alive.  A
-    stack [blocks, rows, cols] is its matrices' rows one after the other; any other tensor has its first dimension as rows.  Without
+    """List of tensors given as dict(w, m, v=None, grads=[...], blocks=0, rate_scale=1.0) as C lays it out, and what keeps the arrays it points to
+    alive.  A stack [blocks, rows, cols] is its matrices' rows one after the other; any other tensor has its first dimension as rows.  Without
     pointers: shapes only."""
-    from torch import float32
-    arr = (spb_muon_tensor * max(1, len(tensors)))()
-    held = array.array("Q", [g.data_ptr() for t in tensors for g in t["grads"]] if pointers else ())
-    at = held.buffer_info()[0]
-    for i, t in enumerate(tensors):
+    stored, packed = _stored(), []
+    held = array.array("Q", [g.data_ptr() for t in tensors for g in t["grads"]]) if pointers else None
+    at = held.buffer_info()[0] if pointers else 0
+    for t in tensors:
         w, blocks = t["w"], t.get("blocks", 0)
-        shape, where, count = w.shape, (0, 0, 0, 0), 0
+        shape, code = w.shape, stored.get(w.dtype)
+        if code is None:
+            _dtype_code(w)                 # says what is stored
+        pw = pm = pv = pg = count = 0
         if pointers:
             m, v, grads = t["m"], t.get("v"), t["grads"]
-            good = w.is_contiguous()
             for x in (m, *grads) if v is None else (m, v, *grads):
-                good = good and x.dtype is float32 and x.shape == shape and x.is_contiguous()
-            if not good:
-                raise ValueError("m, v and gradients are contiguous float32 tensors of the parameter's shape, which is contiguous too")
-            where, count = (w.data_ptr(), m.data_ptr(), 0 if v is None else v.data_ptr(), at), len(grads)
+                if stored.get(x.dtype) != _F32 or x.shape != shape or not x.is_contiguous():
+                    raise ValueError(_MUON_LAYOUT)
+            if not w.is_contiguous():
+                raise ValueError(_MUON_LAYOUT)
+            pw, pm, pv, pg, count = w.data_ptr(), m.data_ptr(), 0 if v is None else v.data_ptr(), at, len(grads)
             at += 8 * count
         dims = len(shape)
         rows = shape[0] * shape[1] if dims == 3 and blocks >= 1 and shape[0] == blocks else shape[0] if dims else 1
-        _MUON.pack_into(arr, i * _MUON.size, *where, rows, w.numel() // rows if rows else 0, t.get("rate_scale", 1.0), count, _dtype_code(w), blocks, 0)
-    return arr, held
+        packed.append(_MUON.pack(pw, pm, pv, pg, rows, w.numel() // rows if rows else 0, t.get("rate_scale", 1.0), count, code, blocks, 0))
+    return b"".join(packed), held
 
 
 def spb_muon_workspace_size(tensors) -> int:
     """Shapes, types and blocks of the tensors are all it looks at."""
-    arr, _ = _muon_tensors(tensors, pointers=False)
     n = C.c_size_t()
-    _check(lib().spb_muon_workspace_size(arr, len(tensors), n))
+    _check(lib().spb_muon_workspace_size(_muon_tensors(tensors, pointers=False)[0], len(tensors), n))
     return n.value
 
 
 def spb_muon_step(tensors, config: spb_muon_config, workspace, workspace_bytes, stream):
-    arr, _held = _muon_tensors(tensors)
-    _check(lib().spb_muon_step(arr, len(tensors), config, _address(workspace), workspace_bytes, stream))
+    listed, _held = _muon_tensors(tensors)
+    _check(lib().spb_muon_step(listed, len(tensors), config, _address(workspace), workspace_bytes, stream))
 
 
 def spb_aggregate_muon_workspace_size(m, blocks) -> int:
