@@ -140,6 +140,10 @@ CASES = {
     "f32_odd": dict(b=2, s=21, hq=2, hk=1, d=27, dtype=torch.float32, layout="odd", sections=(6, 7)),
     "f32_turn": dict(b=2, s=9, hq=3, hk=0, d=12, dtype=torch.float32, sections=(6,), norm=False, interleaved=True),
     "many_tokens": dict(b=4, s=1200, hq=3, hk=1, d=32, sections=(8, 8)),
+    "few_heads": dict(b=3, s=22001, hq=1, hk=0, d=16),
+    "few_heads_turned": dict(b=2, s=9001, hq=2, hk=1, d=40, sections=(10, 10)),
+    "few_heads_general": dict(b=1, s=17001, hq=1, hk=1, d=9, dtype=torch.float32, sections=(3,)),
+    "few_heads_128_pairs": dict(b=1, s=4999, hq=1, hk=0, d=256, sections=(43, 43, 42), far=2 ** 31 - 1),
     "large_values": dict(b=1, s=33, hq=4, hk=4, d=64, loud=1e15, sections=(32,)),
     "small_values": dict(b=1, s=33, hq=4, hk=4, d=64, loud=1e-12, dtype=torch.float32),
 }

@@ -234,6 +234,16 @@ def test_many_tensors_of_all_kinds_at_once():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("sides", [(3, 40), (60, 90), (260, 300)])
+def test_more_shapes_than_a_launch_holds(sides):
+    tensors = [_tensor((sides[0] + i, sides[1]), 1, torch.bfloat16 if i % 2 else torch.float32, 1 + i % 3, seed=40 + i, w=0.0) for i in range(56)]
+    before = [_numpy(t) for t in tensors]
+    _step(tensors)
+    for b, t in zip(before, tensors):
+        _check(b, _numpy(t), t["w"].dtype)
+
+
+@pytest.mark.gpu
 def test_tensors_at_odd_addresses():
     for dtype in (torch.bfloat16, torch.float32):
         for blocks, shape in ((1, (30, 41)), (0, (1229,))):
