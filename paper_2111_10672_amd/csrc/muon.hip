@@ -1339,7 +1339,8 @@ __global__ __launch_bounds__(kThreads) void narrow_apply_kernel(NarrowGroups gro
 // ---- plan -----------------------------------------------------------------------------------------------------------
 
 // What a product of `count` matrices in tiles of `tile` takes, in us, from these kernels' times over 1 to 64 matrices of 64 x 64 to 4096 x 4096: rounds of
-// workgroups over the 256 CUs, each a start and an end (2 to 8 us) and so much for every 64 of k, less where a round is alone.  Tiles of 64 and of 256 have a CU to
+// workgroups over the 256 CUs, each a start and an end (2 to 8 us) and so much for every 64 of k, less where a round is alone.  The short rounds of tiles of 32 run into one
+// another: a tenth or a third of a round on top, not a whole one (one product of 1024 x 1024 x 1024 in bfloat16, 528 tiles: 7 us, with tiles of 64 9).  Tiles of 64 and of 256 have a CU to
 // themselves (rings of 96 and 128 KB); those of 128 share one with another once there are more than CUs (24 products of 1024 x 4096 x 1024: 272 us so, 345 us
 // alone on a ring of four), and have it to themselves before (136 tiles over k = 2048: 26 against 23).  One float32 product of 1024 x 1024 x 1024: tiles
 // of 64 13 us, of 128 24; 16 of them: 175 and 112.  One of 256 x 256 x 784: tiles of 32 6.0 us, of 64 10.5; one bfloat16 product of 512 cubed 4.2 and 6.2, of 2048
@@ -1349,11 +1350,11 @@ double product_cost(long long tiles, int tile, int planes, int k) {
   auto rounds = [&](int at_once) { return (double)((tiles + at_once - 1) / at_once); };
   const bool alone = tiles <= 256;
   if (planes == 2) {
-    if (tile == 32) return alone ? 3.6 + 0.16 * steps : rounds(256) * (3.2 + 0.26 * steps);
+    if (tile == 32) return alone ? 3.6 + 0.16 * steps : (tiles / 256.0 + 0.35) * (3.2 + 0.26 * steps);
     if (tile == 64) return alone ? 4.7 + 0.42 * steps : rounds(256) * (2.0 + 0.56 * steps);
     return rounds(256) * (5.0 + 1.44 * steps);
   }
-  if (tile == 32) return alone ? 2.8 + 0.09 * steps : rounds(512) * (2.0 + 0.24 * steps);
+  if (tile == 32) return alone ? 2.8 + 0.09 * steps : std::max(tiles / 512.0 + 0.1, 1.0) * (2.0 + 0.24 * steps);
   if (tile == 64) return alone ? 4.2 + 0.29 * steps : rounds(256) * (2.8 + 0.29 * steps);
   if (tile == 128) return alone ? 5.0 + 0.6 * steps : rounds(512) * (6.0 + 1.0 * steps);
   return rounds(256) * (8.0 + 1.64 * steps);
