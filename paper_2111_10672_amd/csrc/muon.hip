@@ -1343,15 +1343,16 @@ __global__ __launch_bounds__(kThreads) void narrow_apply_kernel(NarrowGroups gro
 // another: a tenth or a third of a round on top, not a whole one (one product of 1024 x 1024 x 1024 in bfloat16, 528 tiles: 7 us, with tiles of 64 9).  Tiles of 64 and of 256 have a CU to
 // themselves (rings of 96 and 128 KB); those of 128 share one with another once there are more than CUs (24 products of 1024 x 4096 x 1024: 272 us so, 345 us
 // alone on a ring of four), and have it to themselves before (136 tiles over k = 2048: 26 against 23).  One float32 product of 1024 x 1024 x 1024: tiles
-// of 64 13 us, of 128 24; 16 of them: 175 and 112.  One of 256 x 256 x 784: tiles of 32 6.0 us, of 64 10.5; one bfloat16 product of 512 cubed 4.2 and 6.2, of 2048
+// of 64 13 us, of 128 24; 16 of them: 175 and 112.  Symmetric ones in many rounds: 19 matrices
+// of 617 x 1467, both products of a step in tiles of 64 145 us, of 128 126.  One of 256 x 256 x 784: tiles of 32 6.0 us, of 64 10.5; one bfloat16 product of 512 cubed 4.2 and 6.2, of 2048
 // cubed 80 and 55, and in tiles of 128 25.  48 of 768 x 768 x 768: tiles of 128 62 us, of 256 53; their symmetric halves 44 and 53.
-double product_cost(long long tiles, int tile, int planes, int k) {
+double product_cost(int mode, long long tiles, int tile, int planes, int k) {
   const double steps = k / 64;
   auto rounds = [&](int at_once) { return (double)((tiles + at_once - 1) / at_once); };
   const bool alone = tiles <= 256;
   if (planes == 2) {
     if (tile == 32) return alone ? 3.6 + 0.16 * steps : (tiles / 256.0 + 0.35) * (3.2 + 0.26 * steps);
-    if (tile == 64) return alone ? 4.7 + 0.42 * steps : rounds(256) * (2.0 + 0.56 * steps);
+    if (tile == 64) return alone ? 4.7 + 0.42 * steps : rounds(256) * (2.0 + (mode == kGram || mode == kPoly ? 0.7 : 0.56) * steps);
     return rounds(256) * (5.0 + 1.44 * steps);
   }
   if (tile == 32) return alone ? 2.8 + 0.09 * steps : std::max(tiles / 512.0 + 0.1, 1.0) * (2.0 + 0.24 * steps);
@@ -1382,7 +1383,7 @@ int pick_tile(int mode, int planes, int pad, const Sizes& groups, int n, double*
       tiles += tiles_of(mode, groups[i].mp, groups[i].np, tile) * groups[i].count;
       k = std::max(k, mode == kGram ? groups[i].np : groups[i].mp);
     }
-    const double c = product_cost(tiles, tile, planes, k);
+    const double c = product_cost(mode, tiles, tile, planes, k);
     if (tile == 32 || c < least) { best = tile; least = c; }
   }
   if (cost) *cost = least;
