@@ -359,8 +359,12 @@ typedef struct spb_muon_tensor {
 #define SPB_MAX_MATRIX_SIDE 65536
 
 typedef struct spb_muon_config {
-  double lr, rms, momentum, ns_eps;
-  double beta1, beta2, adam_eps, weight_decay;
+  double lr, rms, momentum;    /* finite in float32, and so are weight_decay and what follows from them for a tensor: its rate, 1 - rate weight_decay */
+                               /*   and rate rms sqrt(longer side) */
+  double ns_eps;               /* > 0 */
+  double beta1, beta2;         /* in [0, 1) */
+  double adam_eps;             /* a normal float32 number: at least 1.2e-38 */
+  double weight_decay;
   int64_t step;                /* >= 1: how many steps AdamW's moments have seen, this one included.  (A captured call replays with this value.) */
   int32_t nesterov, ns_steps;  /* ns_steps in 1..16 */
 } spb_muon_config;

@@ -55,7 +55,8 @@ struct Matrix {
   const float* u;          // [rows, cols] dense
   const double* partial;   // [parts] sums of u^2
   int parts, rows, cols, bf16;
-  float keep, step, eps;   // w = keep * w - step * X
+  float keep, step;        // w = keep * w - step * X
+  double eps;
 };
 
 // ---- elementwise half ---------------------------------------------------------------------------------------------
@@ -79,7 +80,8 @@ struct Tensor {
 struct Table {
   Tensor t[kMaxTensors];
   int n, nesterov;
-  float momentum, beta1, beta2, new1, new2, inv_c1, inv_c2, adam_eps, ns_eps;   // new1 = 1 - beta1
+  float momentum, beta1, beta2, new1, new2, inv_c1, inv_c2, adam_eps;   // new1 = 1 - beta1
+  double ns_eps;
 };
 
 __device__ __forceinline__ float bf(uint16_t v) { return __uint_as_float(((uint32_t)v) << 16); }
@@ -201,6 +203,15 @@ __global__ __launch_bounds__(kThreads) void update_kernel(Table tab) {
   }
 }
 
+// A factor on its way to float32 as two: the second is 1 unless the first would leave float32's range, where it takes a power of two.
+struct Factor { float main, lift; };
+__device__ __forceinline__ Factor factor_of(double f) {
+  const double lift = f > 0x1p100 ? 0x1p100 : f < 0x1p-100 ? 0x1p-100 : 1.0;
+  return Factor{(float)(f / lift), (float)lift};
+}
+// by / (|u| + eps) from the sum of u's squares; a u of zeros stays one whatever eps is.
+__device__ __forceinline__ double over_norm(double by, double squares, double eps) { return squares == 0.0 ? 0.0 : by / (sqrt(squares) + eps); }
+
 // ---- matrices of one padded shape -----------------------------------------------------------------------------------
 
 constexpr int kMaxGroups = 24;
@@ -317,14 +328,14 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(Groups groups) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) tile_s[k * 16 + (threadIdx.x >> 4)][(threadIdx.x & 15) * 4 + e] = in[k][e];
   __syncthreads();
-  const float scale = (float)((double)g.sigma / (sqrt((sums[0] + sums[1]) + (sums[2] + sums[3])) + (double)d.eps));
+  const Factor scale = factor_of(over_norm((double)g.sigma, (sums[0] + sums[1]) + (sums[2] + sums[3]), d.eps));
   const size_t plane = (size_t)g.mp * g.np;
   _Float16* x = g.x[0] + mat * PLANES * plane;
   for (int k = threadIdx.x; k < 64 * 8; k += kThreads) {
     const int i = BLOCKS ? (k >> 7) * 16 + (k & 15) : k >> 3, j = BLOCKS ? ((k >> 4) & 7) * 8 : (k & 7) * 8;
     float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (tall ? tile_s[j + e][i] : tile_s[i][j + e]) * scale;
+    for (int e = 0; e < 8; ++e) v[e] = (tall ? tile_s[j + e][i] : tile_s[i][j + e]) * scale.lift * scale.main;
     split8<PLANES>(v, x + (BLOCKS ? place(g.np, i0 + i, j0 + j) : (size_t)(i0 + i) * g.np + j0 + j), plane);
   }
 }
@@ -1084,7 +1095,7 @@ typedef double f64x4 __attribute__((ext_vector_type(4)));
 struct NarrowGroup {
   const Matrix* matrices;
   double* partial;         // [count][slices][tiles][256]: 16 x 16 tiles of u u^T on and below the diagonal
-  float* q;                // [count][shorter][shorter], and behind the matrices [count] factors 1 / (|u| + eps)
+  float* q;                // [count][shorter][shorter], and behind the matrices [count] factors 1 / (|u| + eps) in two
   int shorter, longer, count, tiles, slices, first_block;
 };
 struct NarrowGroups {
@@ -1215,7 +1226,7 @@ __device__ __forceinline__ void narrow_chain(const NarrowGroup& g, int mat, int 
     double s = lane < 16 * M16 ? a[lane * kPitch + lane] : 0.0;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-    if (lane == 0) *norm = 1.0 / (sqrt(s) + (double)g.matrices[mat].eps);
+    if (lane == 0) *norm = over_norm(1.0, s, g.matrices[mat].eps);
   }
   __syncthreads();
   const double inv = *norm;
@@ -1261,7 +1272,7 @@ __device__ __forceinline__ void narrow_chain(const NarrowGroup& g, int mat, int 
   const double* chain = steps == 1 ? b : q;
   float* out = g.q + (size_t)mat * g.shorter * g.shorter;
   for (int e = threadIdx.x; e < g.shorter * g.shorter; e += kChainThreads) out[e] = (float)chain[(e / g.shorter) * kPitch + e % g.shorter];
-  if (threadIdx.x == 0) g.q[(size_t)g.count * g.shorter * g.shorter + mat] = (float)inv;
+  if (threadIdx.x == 0) reinterpret_cast<Factor*>(g.q + (size_t)g.count * g.shorter * g.shorter)[mat] = factor_of(inv);
 }
 
 __global__ __launch_bounds__(kChainThreads) void narrow_chain_kernel(NarrowGroups groups, int steps) {
@@ -1284,7 +1295,7 @@ __global__ __launch_bounds__(kThreads) void narrow_apply_kernel(NarrowGroups gro
   const NarrowGroup g = narrow_group(groups, blockIdx.x, [](const NarrowGroup& q) { return (q.longer + kApply - 1) / kApply; }, mat, part);
   const Matrix d = g.matrices[mat];
   const float* q = g.q + (size_t)mat * g.shorter * g.shorter;
-  const float inv = g.q[(size_t)g.count * g.shorter * g.shorter + mat];
+  const Factor inv = reinterpret_cast<const Factor*>(g.q + (size_t)g.count * g.shorter * g.shorter)[mat];
   constexpr int kRows = kNarrow / 4;
   float qv[kRows];
 #pragma unroll
@@ -1314,7 +1325,9 @@ __global__ __launch_bounds__(kThreads) void narrow_apply_kernel(NarrowGroups gro
     }
 #pragma unroll
   for (int k = 0; k < kRows; ++k) qs[k * 4 + (threadIdx.x >> 6)][threadIdx.x & 63] = qv[k];
-  chunk.park(v, inv, us);
+#pragma unroll
+  for (int k = 0; k < kApply / 4; ++k) v[k] *= inv.lift;
+  chunk.park(v, inv.main, us);
   __syncthreads();
   float acc[4][2] = {};
 #pragma unroll 8
@@ -1544,7 +1557,7 @@ Plan make_plan(const MuonTensor* t, int n) {
     g.x[0] = take(x); g.x[1] = take(x); g.a = take(a); g.b = take(g.pair ? 0 : a);
     if (g.narrow) {   // (many steps take the other way)
       g.partial = take((size_t)g.count * kMaxSlices * narrow_tiles(g.shorter) * 256 * sizeof(double));
-      g.q = take((size_t)g.count * ((size_t)g.shorter * g.shorter + 1) * sizeof(float));
+      g.q = take((size_t)g.count * ((size_t)g.shorter * g.shorter * sizeof(float) + sizeof(Factor)));
     }
     // a power of two that brings entries of the size a flat matrix of norm 1 has to about 1
     g.sigma = std::exp2((float)std::min(14, (int)std::lround(0.5 * std::log2((double)g.mp * g.np))));
@@ -1691,7 +1704,7 @@ hipError_t launch_muon_step(const MuonTensor* tensors, int n, const spb_muon_con
   int i = 0;
   while (i < n) {
     Table tab = {};
-    tab.nesterov = c.nesterov; tab.momentum = (float)c.momentum; tab.adam_eps = (float)c.adam_eps; tab.ns_eps = (float)c.ns_eps;
+    tab.nesterov = c.nesterov; tab.momentum = (float)c.momentum; tab.adam_eps = (float)c.adam_eps; tab.ns_eps = c.ns_eps;
     tab.beta1 = (float)c.beta1; tab.beta2 = (float)c.beta2; tab.new1 = (float)(1.0 - c.beta1); tab.new2 = (float)(1.0 - c.beta2);
     tab.inv_c1 = (float)(1.0 / (1.0 - std::pow(c.beta1, (double)c.step)));
     tab.inv_c2 = (float)(1.0 / (1.0 - std::pow(c.beta2, (double)c.step)));

@@ -2,6 +2,7 @@
 // the host, then the launches.
 #include <algorithm>
 #include <cmath>
+#include <limits>
 #include <new>
 
 #include "model.h"
@@ -81,12 +82,17 @@ int launched(hipError_t e, const char* who) {
   return e == hipErrorInvalidValue ? SPB_ERR_INVALID_ARG : SPB_ERR_HIP;
 }
 
+// Whether a factor that kernels take in float32 stays finite there.
+bool fits_f32(double v) { return std::isfinite((float)v); }
+
 int check_config(const spb_muon_config* c, const char* who) {
   SPB_REQUIRE(c, SPB_ERR_INVALID_ARG, "%s: null configuration", who);
-  SPB_REQUIRE(std::isfinite(c->lr) && std::isfinite(c->rms) && std::isfinite(c->weight_decay) && std::isfinite(c->momentum), SPB_ERR_INVALID_ARG,
-              "%s: lr, rms, momentum and weight_decay must be finite", who);
+  SPB_REQUIRE(fits_f32(c->lr) && fits_f32(c->rms) && fits_f32(c->weight_decay) && fits_f32(c->momentum), SPB_ERR_INVALID_ARG,
+              "%s: lr, rms, momentum and weight_decay must be finite in float32", who);
   SPB_REQUIRE(c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0, SPB_ERR_INVALID_ARG, "%s: beta1 and beta2 must lie in [0, 1)", who);
   SPB_REQUIRE(c->ns_eps > 0.0 && c->adam_eps > 0.0 && std::isfinite(c->ns_eps) && std::isfinite(c->adam_eps), SPB_ERR_INVALID_ARG, "%s: ns_eps and adam_eps must be positive", who);
+  // (ns_eps stays in float64; adam_eps as zero or with few bits would turn moments of zero into 0 / 0)
+  SPB_REQUIRE((float)c->adam_eps >= std::numeric_limits<float>::min(), SPB_ERR_INVALID_ARG, "%s: adam_eps %g is below float32's normal numbers", who, c->adam_eps);
   SPB_REQUIRE(c->step >= 1, SPB_ERR_INVALID_ARG, "%s: step %lld", who, (long long)c->step);
   SPB_REQUIRE(c->ns_steps >= 1 && c->ns_steps <= 16, SPB_ERR_INVALID_ARG, "%s: ns_steps %d outside 1..16", who, c->ns_steps);
   return SPB_OK;
@@ -124,6 +130,16 @@ int check_tensors(const std::vector<spb::MuonTensor>& t, const char* who) {
   }
   std::sort(seen.begin(), seen.end());
   SPB_REQUIRE(std::adjacent_find(seen.begin(), seen.end()) == seen.end(), SPB_ERR_INVALID_ARG, "%s: the same parameter or moment twice", who);
+  return SPB_OK;
+}
+
+// The factors of the parameter and of its update.
+int check_rates(const std::vector<spb::MuonTensor>& t, const spb_muon_config& c, const char* who) {
+  for (size_t i = 0; i < t.size(); ++i) {
+    const double side = t[i].blocks ? std::sqrt((double)std::max(t[i].rows / t[i].blocks, t[i].cols)) : 1.0;
+    SPB_REQUIRE(fits_f32(t[i].rate) && fits_f32(1.0 - t[i].rate * c.weight_decay) && fits_f32(t[i].rate * c.rms * side), SPB_ERR_INVALID_ARG,
+                "%s: rate %g of tensor %zu leaves float32", who, t[i].rate, i);
+  }
   return SPB_OK;
 }
 
@@ -263,6 +279,7 @@ int spb_muon_step(const spb_muon_tensor* tensors, int32_t n, const spb_muon_conf
       }
     }
     if (int rc = check_tensors(t, who)) return rc;
+    if (int rc = check_rates(t, *config, who)) return rc;
     if (int rc = check_workspace(workspace, workspace_bytes, spb::muon_workspace_size(t.data(), n), who)) return rc;
     return launched(spb::launch_muon_step(t.data(), n, *config, workspace, static_cast<hipStream_t>(stream)), who);
   });
@@ -337,6 +354,7 @@ int spb_aggregate_muon(spb_model* m, int32_t n_workers, const int32_t* depths, v
     }
     if (int rc = check_workspace(workspace, workspace_bytes, spb::muon_workspace_size(t.data(), (int)t.size()), who)) return rc;
     if (int rc = check_tensors(t, who)) return rc;
+    if (int rc = check_rates(t, *config, who)) return rc;
     return launched(spb::launch_muon_step(t.data(), (int)t.size(), *config, workspace, static_cast<hipStream_t>(stream)), who);
   });
 }

@@ -1,0 +1,111 @@
+"""The optimiser step at the ends of its numbers: zeros, gradients next to both ends of float32, and factors that float32 does not hold.  Tolerances: muon_bounds.py."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2111_10672_amd as spb
+from muon_bounds import U, check_matrices
+from paper_2111_10672_amd.binding import _check
+from test_host_streams import run, runtime  # noqa: F401
+from test_muon import HYPER, _numpy, _step, _tensor
+
+# on the Gram matrix, in two launches a step, in three
+SHAPES = [(20, 24), (24, 20), (70, 90), (300, 320)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_a_gradient_of_zeros_leaves_only_the_decay(shape, dtype):
+    """Whatever ns_eps: 0 / (0 + eps) is 0."""
+    for eps in (5e-324, 1e-300, 1e-50, 1e-40, 1e-35, 1e-7, 1e300):
+        t = _tensor(shape, 1, dtype, 1, seed=5)
+        t["m"].zero_()
+        t["grads"][0].zero_()
+        before = t["w"].double()
+        _step([t], {**HYPER, "ns_eps": eps})
+        want = before * (1.0 - HYPER["lr"] * HYPER["weight_decay"])
+        half = 2.0 ** -8 if dtype == torch.bfloat16 else U
+        assert bool(((t["w"].double() - want).abs() <= (half + 4 * U) * before.abs()).all()), eps
+        assert not t["m"].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_gradients_next_to_the_ends_of_float32(shape, dtype):
+    """1 / |u| or the scale that follows from it leaves float32, u does not: the update is that of any other size.  (Without momentum, so that u is the gradient itself.)"""
+    for scale, eps in ((1e-42, 1e-300), (1e-39, 5e-324), (1e-36, 1e-45), (3e37, 1e-7)):
+        hyper = {**HYPER, "momentum": 0.0, "nesterov": False, "ns_eps": eps}
+        t = _tensor(shape, 1, dtype, 1, seed=6, w=0.0, scale=scale)
+        t["m"].zero_()
+        before = _numpy(t)
+        _step([t], hyper)
+        check_matrices(before, _numpy(t), dtype, hyper)
+
+
+@pytest.mark.gpu
+def test_moments_of_zero_under_the_smallest_adam_eps():
+    for dtype in (torch.bfloat16, torch.float32):
+        t = _tensor((515,), 0, dtype, 1, seed=7)
+        for x in (t["m"], t["v"], t["grads"][0]):
+            x[::2] = 0.0
+        before = t["w"].double()
+        _step([t], {**HYPER, "adam_eps": 1.2e-38})
+        assert bool(t["w"].isfinite().all())
+        half = 2.0 ** -8 if dtype == torch.bfloat16 else U
+        want = before * (1.0 - HYPER["lr"] * HYPER["weight_decay"])
+        assert bool(((t["w"].double() - want).abs() <= (half + 4 * U) * before.abs())[::2].all())
+
+
+# ---- refusals: all found on the host ----------------------------------------------------------------------------------
+
+def _call(config=None, **patch):
+    grads = (C.c_void_p * 1)(1 << 20)
+    t = (spb.binding.spb_muon_tensor * 1)()
+    t[0].w, t[0].m, t[0].v, t[0].grads = 1 << 12, 1 << 13, 1 << 14, C.cast(grads, C.POINTER(C.c_void_p))
+    t[0].rows, t[0].cols, t[0].rate_scale, t[0].count, t[0].dtype, t[0].blocks = 6, 5, 1.0, 1, 1, 1
+    for k, v in patch.items():
+        setattr(t[0], k, v)
+    _check(spb.lib().spb_muon_step(t, 1, C.byref(spb.muon_config(**{**HYPER, **(config or {})})), 1 << 21, 1 << 20, None))
+
+
+@pytest.mark.parametrize("config,patch", [(dict(lr=1e39), {}), (dict(rms=1e39), {}), (dict(momentum=-1e39), {}), (dict(weight_decay=1e39), {}), (dict(lr=1e20, rms=1e20), {}),
+                                          (dict(lr=1e20, weight_decay=1e20), {}), (dict(lr=1e20, weight_decay=1e20), dict(blocks=0)), ({}, dict(rate_scale=1e300)),
+                                          (dict(rms=2e38), dict(rate_scale=100.0)), (dict(adam_eps=1e-39), dict(blocks=0)), (dict(adam_eps=1e-50), dict(blocks=0)),
+                                          (dict(adam_eps=1e-39), {})])
+def test_factors_that_float32_does_not_hold_are_refused(config, patch):
+    with pytest.raises(spb.SpbError) as e:
+        _call(config, **patch)
+    assert e.value.code == -1 and "spb_muon_step" in str(e.value)
+
+
+def test_the_server_step_refuses_them_too():
+    import workloads as wl
+    m = spb.spb_model_create(spb.desc_from_config(wl.get_config("ragged_mlp_bf16")))
+    try:
+        n = spb.spb_param_count(m)
+        spb.spb_bind_params(m, [(i + 1) << 32 for i in range(n)])
+        blocks = [int(len(spb.spb_param_info(m, i)["shape"]) > 1) for i in range(n)]
+        size = spb.spb_aggregate_muon_workspace_size(m, blocks)
+        at = lambda k: [(k << 44) + (i << 32) for i in range(n)]
+        for config in (dict(lr=1e39), dict(lr=1e20, rms=1e20), dict(adam_eps=1e-40)):
+            with pytest.raises(spb.SpbError) as e:
+                spb.spb_aggregate_muon(m, [4], [at(1)], blocks, at(2), at(3), spb.muon_config(**{**HYPER, **config}), True, 1 << 60, size, 0)
+            assert e.value.code == -1, config
+    finally:
+        spb.spb_model_destroy(m)
+
+
+def test_factors_at_the_ends_of_float32_are_taken(run):  # noqa: F811
+    run("""
+    def call(config, blocks=1):
+        grads, t = (C.c_void_p * 1)(1 << 20), (spb.binding.spb_muon_tensor * 1)()
+        t[0].w, t[0].m, t[0].v, t[0].grads = 1 << 12, 1 << 13, 1 << 14, C.cast(grads, C.POINTER(C.c_void_p))
+        t[0].rows, t[0].cols, t[0].rate_scale, t[0].count, t[0].dtype, t[0].blocks = 6, 5, 1.0, 1, 1, blocks
+        spb.binding._check(spb.lib().spb_muon_step(t, 1, C.byref(spb.muon_config(**config)), 1 << 21, 1 << 20, None))
+    for config in (dict(lr=1e30), dict(lr=0.0), dict(lr=1e-300), dict(lr=0.1, ns_eps=5e-324), dict(lr=0.1, ns_eps=1e300), dict(lr=0.1, adam_eps=1.2e-38), dict(lr=0.1, beta1=1 - 1e-9)):
+        call(config)
+        call(config, 0)
+    """)
