@@ -369,7 +369,8 @@ typedef struct spb_muon_config {
   int32_t nesterov, ns_steps;  /* ns_steps in 1..16 */
 } spb_muon_config;
 
-/* Bytes of workspace of a step over these tensors: 0 if none is a matrix.  Device pointers are not looked at. */
+/* Bytes of workspace of a step over these tensors: 0 if none is a matrix.  Device pointers are not looked at.  Errors: INVALID_ARG (null, shapes
+ * that the step refuses). */
 int spb_muon_workspace_size(const spb_muon_tensor* tensors, int32_t n, size_t* bytes);
 
 /* One step over n tensors, enqueued on `stream`; needs no model, allocates nothing and may be captured into a HIP graph.

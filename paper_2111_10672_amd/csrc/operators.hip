@@ -117,11 +117,16 @@ int check_workspace(const void* workspace, size_t bytes, size_t need, const char
   return SPB_OK;
 }
 
-int check_tensors(const std::vector<spb::MuonTensor>& t, const char* who) {
+// Before anything is planned: the plan counts matrices in 32 bits.
+int check_total(const std::vector<spb::MuonTensor>& t, const char* who) {
   __int128 padded = 0;
   for (const auto& x : t)
     if (x.blocks) padded += (__int128)x.blocks * ((x.rows / x.blocks + 255) / 256 * 256) * ((x.cols + 255) / 256 * 256);
   SPB_REQUIRE(padded <= kMostEntries, SPB_ERR_INVALID_ARG, "%s: too many matrices for one call", who);
+  return SPB_OK;
+}
+
+int check_tensors(const std::vector<spb::MuonTensor>& t, const char* who) {
   std::vector<const void*> seen;
   for (const auto& x : t) {
     seen.push_back(x.w);
@@ -254,6 +259,7 @@ int spb_muon_workspace_size(const spb_muon_tensor* tensors, int32_t n, size_t* b
   return guarded(who, [&] {
     std::vector<spb::MuonTensor> t;
     if (int rc = tensors_of(tensors, n, &t, who)) return rc;
+    if (int rc = check_total(t, who)) return rc;
     *bytes = spb::muon_workspace_size(t.data(), n);
     return SPB_OK;
   });
@@ -265,6 +271,7 @@ int spb_muon_step(const spb_muon_tensor* tensors, int32_t n, const spb_muon_conf
   return guarded(who, [&] {
     std::vector<spb::MuonTensor> t;
     if (int rc = tensors_of(tensors, n, &t, who)) return rc;
+    if (int rc = check_total(t, who)) return rc;
     for (int i = 0; i < n; ++i) {
       const spb_muon_tensor& s = tensors[i];
       const size_t size = s.dtype == SPB_DTYPE_F32 ? 4 : 2;
@@ -301,7 +308,7 @@ static int suffix_of(const spb::Model& im, const int32_t* blocks, int unit, std:
     d.blocks = blocks[i]; d.dtype = im.params[i].dtype;
     t->push_back(d);
   }
-  return SPB_OK;
+  return check_total(*t, who);
 }
 
 int spb_aggregate_muon_workspace_size(const spb_model* m, const int32_t* blocks, size_t* bytes) {
@@ -352,6 +359,7 @@ int spb_aggregate_muon(spb_model* m, int32_t n_workers, const int32_t* depths, v
       d.rate = scale_lr ? config->lr * d.count / n_workers : config->lr;
       t.push_back(d);
     }
+    if (int rc = check_total(t, who)) return rc;
     if (int rc = check_workspace(workspace, workspace_bytes, spb::muon_workspace_size(t.data(), (int)t.size()), who)) return rc;
     if (int rc = check_tensors(t, who)) return rc;
     if (int rc = check_rates(t, *config, who)) return rc;

@@ -109,3 +109,34 @@ def test_factors_at_the_ends_of_float32_are_taken(run):  # noqa: F811
         call(config)
         call(config, 0)
     """)
+
+
+def test_more_matrices_than_a_step_takes_have_no_workspace_size():
+    """2^31 of them and more would not be counted right."""
+    t = (spb.binding.spb_muon_tensor * 2)()
+    size = C.c_size_t(77)
+    for x in t:
+        x.rows, x.cols, x.dtype, x.blocks = 1 << 30, 1, 1, 1 << 30
+    for n in (1, 2):
+        with pytest.raises(spb.SpbError) as e:
+            _check(spb.lib().spb_muon_workspace_size(t, n, C.byref(size)))
+        assert e.value.code == -1 and size.value == 77
+    t[0].rows = t[0].blocks = 1 << 17                                   # 2^17 of 256 x 256, padded: as many as a step takes
+    _check(spb.lib().spb_muon_workspace_size(t, 1, C.byref(size)))
+    assert size.value > (1 << 17) * 4
+    with pytest.raises(spb.SpbError) as e:
+        _call(rows=1 << 18, cols=1, blocks=1 << 18)
+    assert e.value.code == -1 and "too many" in str(e.value)
+
+
+def test_the_server_step_of_more_matrices_than_it_takes_has_no_workspace_size():
+    import workloads as wl
+    cfg = dict(wl.get_config("ragged_mlp_bf16"), dims=[8, 1 << 16, 1 << 16])
+    m = spb.spb_model_create(spb.desc_from_config(cfg))
+    try:
+        blocks = [1 << 16 if len(spb.spb_param_info(m, i)["shape"]) > 1 else 0 for i in range(spb.spb_param_count(m))]
+        with pytest.raises(spb.SpbError) as e:
+            spb.spb_aggregate_muon_workspace_size(m, blocks)
+        assert e.value.code == -1
+    finally:
+        spb.spb_model_destroy(m)
