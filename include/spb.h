@@ -375,7 +375,8 @@ int spb_muon_workspace_size(const spb_muon_tensor* tensors, int32_t n, size_t* b
 
 /* One step over n tensors, enqueued on `stream`; needs no model, allocates nothing and may be captured into a HIP graph.
  *   workspace  device, 256-byte aligned, until the call has completed on the device; NULL if the size is 0
- * Errors: INVALID_ARG (null or misaligned pointers, the same w, m or v twice, values outside their ranges), WORKSPACE, HIP. */
+ * What is written (each w, m and v, the workspace) overlaps neither one another nor a gradient; gradients may be the same.
+ * Errors: INVALID_ARG (null, misaligned or overlapping pointers, values outside their ranges), WORKSPACE, HIP. */
 int spb_muon_step(const spb_muon_tensor* tensors, int32_t n, const spb_muon_config* config, void* workspace, size_t workspace_bytes, void* stream);
 
 /* spb_aggregate_update with the step above in place of SGD: same workers, depths, averaging and rate scaling.

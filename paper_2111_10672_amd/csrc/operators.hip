@@ -126,15 +126,28 @@ int check_total(const std::vector<spb::MuonTensor>& t, const char* who) {
   return SPB_OK;
 }
 
-int check_tensors(const std::vector<spb::MuonTensor>& t, const char* who) {
-  std::vector<const void*> seen;
+// Nothing that a step writes may lie in anything else of it: workgroups take tensors, and parts of them, in any order.
+int check_places(const std::vector<spb::MuonTensor>& t, const void* workspace, size_t workspace_bytes, const char* who) {
+  struct Span { uintptr_t from, to; };
+  auto span = [](const void* p, size_t bytes) { return Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes}; };
+  std::vector<Span> written;
+  written.reserve(3 * t.size() + 1);
   for (const auto& x : t) {
-    seen.push_back(x.w);
-    seen.push_back(x.m);
-    if (x.v) seen.push_back(x.v);
+    const size_t n = (size_t)(x.rows * x.cols);
+    written.push_back(span(x.w, n * (x.dtype == spb::DType::F32 ? 4 : 2)));
+    written.push_back(span(x.m, n * 4));
+    if (x.v) written.push_back(span(x.v, n * 4));
   }
-  std::sort(seen.begin(), seen.end());
-  SPB_REQUIRE(std::adjacent_find(seen.begin(), seen.end()) == seen.end(), SPB_ERR_INVALID_ARG, "%s: the same parameter or moment twice", who);
+  if (workspace_bytes) written.push_back(span(workspace, workspace_bytes));
+  std::sort(written.begin(), written.end(), [](const Span& a, const Span& b) { return a.from < b.from; });
+  for (size_t i = 1; i < written.size(); ++i)
+    SPB_REQUIRE(written[i].from >= written[i - 1].to, SPB_ERR_INVALID_ARG, "%s: a parameter, moment or the workspace lies in another", who);
+  for (size_t i = 0; i < t.size(); ++i)
+    for (int j = 0; j < t[i].count; ++j) {
+      const Span g = span(t[i].g[j], (size_t)(t[i].rows * t[i].cols) * 4);
+      const auto at = std::upper_bound(written.begin(), written.end(), g.from, [](uintptr_t from, const Span& s) { return from < s.to; });
+      SPB_REQUIRE(at == written.end() || at->from >= g.to, SPB_ERR_INVALID_ARG, "%s: gradient %d of tensor %zu lies in what the step writes", who, j, i);
+    }
   return SPB_OK;
 }
 
@@ -285,9 +298,10 @@ int spb_muon_step(const spb_muon_tensor* tensors, int32_t n, const spb_muon_conf
         t[i].g[j] = s.grads[j];
       }
     }
-    if (int rc = check_tensors(t, who)) return rc;
     if (int rc = check_rates(t, *config, who)) return rc;
-    if (int rc = check_workspace(workspace, workspace_bytes, spb::muon_workspace_size(t.data(), n), who)) return rc;
+    const size_t need = spb::muon_workspace_size(t.data(), n);
+    if (int rc = check_workspace(workspace, workspace_bytes, need, who)) return rc;
+    if (int rc = check_places(t, workspace, need, who)) return rc;
     return launched(spb::launch_muon_step(t.data(), n, *config, workspace, static_cast<hipStream_t>(stream)), who);
   });
 }
@@ -360,8 +374,9 @@ int spb_aggregate_muon(spb_model* m, int32_t n_workers, const int32_t* depths, v
       t.push_back(d);
     }
     if (int rc = check_total(t, who)) return rc;
-    if (int rc = check_workspace(workspace, workspace_bytes, spb::muon_workspace_size(t.data(), (int)t.size()), who)) return rc;
-    if (int rc = check_tensors(t, who)) return rc;
+    const size_t need = spb::muon_workspace_size(t.data(), (int)t.size());
+    if (int rc = check_workspace(workspace, workspace_bytes, need, who)) return rc;
+    if (int rc = check_places(t, workspace, need, who)) return rc;
     if (int rc = check_rates(t, *config, who)) return rc;
     return launched(spb::launch_muon_step(t.data(), (int)t.size(), *config, workspace, static_cast<hipStream_t>(stream)), who);
   });

@@ -140,3 +140,36 @@ def test_the_server_step_of_more_matrices_than_it_takes_has_no_workspace_size():
         assert e.value.code == -1
     finally:
         spb.spb_model_destroy(m)
+
+
+# Two float32 tensors of 6 x 5 and 40 entries: a matrix and one that AdamW takes.
+PLACES = dict(w0=1 << 16, m0=2 << 16, g0=3 << 16, w1=4 << 16, m1=5 << 16, v1=6 << 16, g1=7 << 16, ws=8 << 16)
+
+
+def _places(lib, **patch):
+    p = {**PLACES, **patch}
+    t, keep = (spb.binding.spb_muon_tensor * 2)(), []
+    for x, g, fields in ((t[0], "g0", dict(w=p["w0"], m=p["m0"], rows=6, cols=5, blocks=1)), (t[1], "g1", dict(w=p["w1"], m=p["m1"], v=p["v1"], rows=40, cols=1, blocks=0))):
+        keep.append((C.c_void_p * 1)(p[g]))
+        for k, v in dict(fields, rate_scale=1.0, count=1, dtype=0, grads=C.cast(keep[-1], C.POINTER(C.c_void_p))).items():
+            setattr(x, k, v)
+    size = C.c_size_t()
+    _check(lib.spb_muon_workspace_size(t, 2, C.byref(size)))
+    _check(lib.spb_muon_step(t, 2, C.byref(spb.muon_config(**HYPER)), p["ws"], size.value, None))
+
+
+@pytest.mark.parametrize("patch", [dict(m0=PLACES["w0"]), dict(m0=PLACES["w0"] + 116), dict(w1=PLACES["m0"] + 4), dict(v1=PLACES["w1"] + 156), dict(w1=PLACES["w0"] - 156),
+                                   dict(ws=PLACES["w0"] - 256), dict(w0=PLACES["ws"] + 256), dict(g0=PLACES["m1"]), dict(g0=PLACES["v1"] + 156), dict(g1=PLACES["w0"] - 156),
+                                   dict(g0=PLACES["m0"]), dict(g1=PLACES["ws"] + 64)])
+def test_tensors_that_lie_in_one_another_are_refused(patch):
+    with pytest.raises(spb.SpbError) as e:
+        _places(spb.lib(), **patch)
+    assert e.value.code == -1 and "lies in" in str(e.value), patch
+
+
+def test_tensors_side_by_side_and_gradients_of_one_place_are_taken(run):  # noqa: F811
+    import inspect
+    run(f"PLACES, HYPER = {PLACES!r}, {HYPER!r}\nfrom paper_2111_10672_amd.binding import _check\n" + inspect.getsource(_places) + """
+for patch in (dict(), dict(m0=PLACES["w0"] + 120), dict(w1=PLACES["w0"] - 160), dict(g1=PLACES["w0"] - 160), dict(g0=PLACES["g1"]), dict(g0=PLACES["v1"] + 160)):
+    _places(spb.lib(), **patch)
+""")
