@@ -65,6 +65,14 @@ int check_strides(const spb_heads_desc* d, const int64_t* s, bool result, const 
   return SPB_OK;
 }
 
+// A result at an input's address takes that input's place row by row.
+int check_in_place(const spb_heads_desc* d, const void* in, const int64_t* s, const void* out, const int64_t* o, const char* name, const char* who) {
+  if (in != out) return SPB_OK;
+  const long long extent[3] = {d->batch, d->seq, (long long)d->heads_q + d->heads_k};
+  for (int i = 0; i < 3; ++i) SPB_REQUIRE(extent[i] <= 1 || s[i] == o[i], SPB_ERR_INVALID_ARG, "%s: in place of %s with other strides", who, name);
+  return SPB_OK;
+}
+
 spb::HeadsProblem heads_problem(const spb_heads_desc* d, const int32_t* pos, int64_t pos_axis_stride, int64_t pos_batch_stride) {
   spb::HeadsProblem q;
   q.dtype = d->dtype == SPB_DTYPE_F32 ? spb::DType::F32 : spb::DType::BF16;
@@ -212,6 +220,7 @@ int spb_heads_forward(const spb_heads_desc* d, const void* x, void* y, const int
   if (d->batch == 0 || d->seq == 0) return SPB_OK;
   const size_t size = d->dtype == SPB_DTYPE_F32 ? 4 : 2;
   SPB_REQUIRE(x && y && aligned(x, size) && aligned(y, size), SPB_ERR_INVALID_ARG, "%s: x or y null or misaligned", who);
+  if (int rc = check_in_place(d, x, d->x_stride, y, d->y_stride, "x", who)) return rc;
   SPB_REQUIRE(!d->rotary.pairs || (pos && aligned(pos, 4)), SPB_ERR_INVALID_ARG, "%s: a rotation needs positions", who);
   SPB_REQUIRE(!d->norm || (gamma && aligned(gamma, size) && aligned(beta, size)), SPB_ERR_INVALID_ARG, "%s: gamma null, or gamma or beta misaligned", who);
   return guarded(who, [&] {
@@ -242,6 +251,11 @@ int spb_heads_backward(const spb_heads_desc* d, const void* x, const void* dy, v
   const bool empty = d->batch == 0 || d->seq == 0;
   const size_t size = d->dtype == SPB_DTYPE_F32 ? 4 : 2;
   SPB_REQUIRE(empty || (dy && dx && aligned(dy, size) && aligned(dx, size)), SPB_ERR_INVALID_ARG, "%s: dy or dx null or misaligned", who);
+  if (!empty) {
+    if (int rc = check_in_place(d, dy, d->y_stride, dx, d->dx_stride, "dy", who)) return rc;
+    if (d->norm)
+      if (int rc = check_in_place(d, x, d->x_stride, dx, d->dx_stride, "x", who)) return rc;
+  }
   SPB_REQUIRE(empty || !d->rotary.pairs || (pos && aligned(pos, 4)), SPB_ERR_INVALID_ARG, "%s: a rotation needs positions", who);
   if (d->norm) {
     SPB_REQUIRE(empty || (x && aligned(x, size)), SPB_ERR_INVALID_ARG, "%s: with norm x is needed", who);
