@@ -65,6 +65,7 @@ class spb_sched_task(C.Structure):
                 ("moved", C.c_int32), ("start", C.c_double), ("end", C.c_double), ("held_until", C.c_double)]
 
 
+_F32 = DTYPES["f32"]
 SPB_MAX_HEAD_DIM, SPB_MAX_PAIRS, SPB_MAX_AXES, SPB_MAX_MATRIX_SIDE = 256, 128, 4, 65536
 
 
@@ -296,25 +297,28 @@ def spb_aggregate_update(m, depths, worker_grads, velocity, lr, momentum, weight
                                       int(bool(scale_lr)), C.c_void_p(stream)))
 
 
-_NO_SECTIONS = array.array("i", [0])
+_COUNTS = [struct.Struct(f"<{n}i") for n in range(SPB_MAX_AXES + 2)]      # (one more than there are axes: refused in C)
 
 
 def spb_rotary_sections(sections, base=10000.0, own_ladder=False, interleaved=False) -> spb_rotary:
     """Rotary description: sections[a] pairs for axis a; see spb.h for the frequencies."""
-    out = spb_rotary()
-    counts = array.array("i", sections) or _NO_SECTIONS
-    _check(lib().spb_rotary_sections(out, len(sections), counts.buffer_info()[0], base, 1 if own_ladder else 0, 1 if interleaved else 0))
+    out, n = spb_rotary(), len(sections)
+    counts = _COUNTS[n].pack(*sections) if n < len(_COUNTS) else b""
+    code = lib().spb_rotary_sections(out, n, counts, base, 1 if own_ladder else 0, 1 if interleaved else 0)
+    if code:
+        _check(code)
     return out
 
 
-_STORED = None      # torch's type -> dtype code (torch is imported by whoever has a tensor)
+_STORED, _TYPES, _INT32 = None, {}, None      # torch's type -> dtype code, the other way round, torch's int32 (torch is imported by whoever has a tensor)
 
 
 def _stored():
-    global _STORED
+    global _STORED, _INT32
     if _STORED is None:
         import torch
-        _STORED = {torch.float32: DTYPES["f32"], torch.bfloat16: DTYPES["bf16"]}
+        _STORED, _INT32 = {torch.float32: DTYPES["f32"], torch.bfloat16: DTYPES["bf16"]}, torch.int32
+        _TYPES.update((code, t) for t, code in _STORED.items())
     return _STORED
 
 
@@ -327,13 +331,8 @@ def _dtype_code(t) -> int:
 
 # Filled in C in one go: field by field through ctypes a description took 12 us, twice the small kernels behind it.
 _HEADS = struct.Struct("<7if9q")       # spb_heads_desc up to its rotary
+_HEADS_READ = struct.Struct("<7if9q4i")    # and the rotary's pairs, interleaved, axes and reserved
 assert _HEADS.size == spb_heads_desc.rotary.offset
-
-
-def _like(t, x, shape, name):
-    if t.shape != shape or t.dtype is not x.dtype:
-        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, x is {tuple(shape)} of {x.dtype}")
-    return t.stride()
 
 
 def heads_desc(x, heads_q, y=None, dx=None, norm=False, eps=1e-5, rotary=None) -> spb_heads_desc:
@@ -341,43 +340,80 @@ def heads_desc(x, heads_q, y=None, dx=None, norm=False, eps=1e-5, rotary=None) -
     [batch, seq, heads, head_dim] of one dtype and any strides but that of the head's elements.  The first heads_q heads are queries, the
     rest keys.  y and dx default to x's strides."""
     d = spb_heads_desc()
-    shape, sx = x.shape, x.stride()
+    shape, dtype, sx = x.shape, x.dtype, x.stride()
     batch, seq, heads, dim = shape
     sy = sd = sx
     if y is not None:
-        sy = _like(y, x, shape, "y")
+        if y.shape != shape or y.dtype is not dtype:
+            raise ValueError(f"y: {tuple(y.shape)} of {y.dtype}, x is {tuple(shape)} of {dtype}")
+        sy = y.stride()
     if dx is not None:
-        sd = _like(dx, x, shape, "dx")
+        if dx.shape != shape or dx.dtype is not dtype:
+            raise ValueError(f"dx: {tuple(dx.shape)} of {dx.dtype}, x is {tuple(shape)} of {dtype}")
+        sd = dx.stride()
     if dim > 1 and not sx[3] == sy[3] == sd[3] == 1:
         raise ValueError("the elements of a head must be contiguous")
-    _HEADS.pack_into(d, 0, _dtype_code(x), batch, seq, heads_q, heads - heads_q, dim, 1 if norm else 0, eps, sx[0], sx[1], sx[2], sy[0], sy[1], sy[2],
+    code = _stored().get(dtype)
+    if code is None:
+        _dtype_code(x)                 # says what is stored
+    _HEADS.pack_into(d, 0, code, batch, seq, heads_q, heads - heads_q, dim, 1 if norm else 0, eps, sx[0], sx[1], sx[2], sy[0], sy[1], sy[2],
                      sd[0], sd[1], sd[2])
     if rotary is not None:
         d.rotary = rotary
     return d
 
 
-def _positions(desc, pos):
+def _on(t, device, name):
+    """Address of a tensor that has to lie on the GPU `device`, or None, or an address as it is."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.get_device() != device or device < 0:
+        raise ValueError(f"{name} is on {t.device}, not on {'GPU ' + str(device) if device >= 0 else 'a GPU'}")
+    return t.data_ptr()
+
+
+def _described(f, device, *tensors):
+    """Raises unless every (tensor, where its strides are in the description, name) is what the description f says, on the GPU `device`; a stride that nothing steps by may be another."""
+    _stored()
+    shape, dtype = (f[1], f[2], f[3] + f[4], f[5]), _TYPES.get(f[0])
+    for t, at, name in tensors:
+        steps = (*f[at:at + 3], 1)
+        if t.shape != shape or t.dtype is not dtype or any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), steps)):
+            raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype} with strides {t.stride()}, described are {shape} of {dtype} with strides {steps}")
+    for t, _at, name in sorted(tensors, key=lambda t: t[0].get_device()):      # (host memory first)
+        _on(t, device, name)
+
+
+def _positions(axes, batch, seq, pos):
     """(address, axis stride, batch stride) of positions [axes, batch, seq], int32; a batch dimension of 1 serves every sequence."""
-    if pos is None:
-        return None, 0, 0
-    import torch
-    shape = pos.shape
-    if pos.dtype is not torch.int32 or len(shape) != 3:
+    shape, stride = pos.shape, pos.stride()
+    if len(shape) != 3 or _stored() and pos.dtype is not _INT32:
         raise ValueError(f"positions are int32 [axes, batch, seq], not {pos.dtype} {tuple(shape)}")
-    (axes, batch, seq), (by_axis, by_batch, by_token) = shape, pos.stride()
-    if axes < desc.rotary.axes or (batch != 1 and batch != desc.batch) or seq != desc.seq or (by_token != 1 and seq > 1):
-        raise ValueError(f"positions {tuple(shape)} (last stride {by_token}) for {desc.rotary.axes} axes of {desc.batch} x {desc.seq} tokens")
-    return pos.data_ptr(), by_axis, 0 if batch == 1 else by_batch
+    has, by, long = shape
+    if has < axes or (by != 1 and by != batch) or long != seq or (stride[2] != 1 and seq > 1):
+        raise ValueError(f"positions {tuple(shape)} (last stride {stride[2]}) for {axes} axes of {batch} x {seq} tokens")
+    return pos.data_ptr(), stride[0], 0 if by == 1 else stride[1]
 
 
-def _weights(desc, t, name, dtype):
+def _weights(t, shape, code, device, name):
     """Address of a [rows of weights, head_dim] tensor, dense."""
     if t is None:
         return None
-    shape = (2 if desc.heads_k else 1, desc.head_dim)
-    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, contiguous {shape} of {dtype} wanted")
+    if t.shape != shape or t.dtype is not _TYPES.get(code) or not t.is_contiguous():
+        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, contiguous {shape} of {_TYPES.get(code)} wanted")
+    if t.get_device() != device:
+        _on(t, device, name)
+    return t.data_ptr()
+
+
+def _workspace(t, size, device):
+    """Address of a workspace tensor of at least `size` bytes."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.nbytes < size:
+        raise ValueError(f"the workspace has {t.nbytes} bytes, not {size}")
+    if t.get_device() != device:
+        _on(t, device, "the workspace")
     return t.data_ptr()
 
 
@@ -385,35 +421,68 @@ def _address(t):
     return None if t is None else t if isinstance(t, int) else t.data_ptr()
 
 
+_NOWHERE = None, 0, 0
+
+
 def spb_heads_forward(desc, x, y, pos, gamma, beta, stream):
-    where, by_axis, by_batch = _positions(desc, pos)
-    _check(lib().spb_heads_forward(desc, x.data_ptr(), y.data_ptr(), where, by_axis, by_batch, _weights(desc, gamma, "gamma", x.dtype),
-                                   _weights(desc, beta, "beta", x.dtype), stream))
+    """x and y as described (see heads_desc), all on one GPU."""
+    f, device, sx, sy = _HEADS_READ.unpack_from(desc), x.get_device(), x.stride(), y.stride()
+    if not (x.shape == y.shape == (f[1], f[2], f[3] + f[4], f[5]) and sx[:3] == f[8:11] and sy[:3] == f[11:14] and sx[3] == sy[3] == 1 and y.get_device() == device >= 0
+            and x.dtype is y.dtype is _TYPES.get(f[0])):
+        _described(f, device, (x, 8, "x"), (y, 11, "y"))
+    if pos is None:
+        where, by_axis, by_batch = _NOWHERE
+    else:
+        where, by_axis, by_batch = _positions(f[19], f[1], f[2], pos)
+        if pos.get_device() != device:
+            _on(pos, device, "positions")
+    rc = lib().spb_heads_forward(desc, x.data_ptr(), y.data_ptr(), where, by_axis, by_batch, None if gamma is None else _weights(gamma, (2 if f[4] else 1, f[5]), f[0], device, "gamma"),
+                                 None if beta is None else _weights(beta, (2 if f[4] else 1, f[5]), f[0], device, "beta"), stream)
+    if rc:
+        _check(rc)
 
 
 def spb_heads_workspace_size(desc) -> int:
     n = C.c_size_t()
-    _check(lib().spb_heads_workspace_size(desc, C.byref(n)))
+    rc = lib().spb_heads_workspace_size(desc, n)
+    if rc:
+        _check(rc)
     return n.value
 
 
 def spb_heads_backward(desc, x, dy, dx, pos, gamma, dgamma, dbeta, workspace, workspace_bytes, stream):
-    import torch
-    where, by_axis, by_batch = _positions(desc, pos)
-    _check(lib().spb_heads_backward(desc, _address(x), _address(dy), _address(dx), where, by_axis, by_batch, _weights(desc, gamma, "gamma", dy.dtype),
-                                    _weights(desc, dgamma, "dgamma", torch.float32), _weights(desc, dbeta, "dbeta", torch.float32), _address(workspace),
-                                    workspace_bytes, stream))
+    """x, dy and dx as described (see heads_desc), all on one GPU; x is not looked at without norm."""
+    f, device, sy, sd = _HEADS_READ.unpack_from(desc), dy.get_device(), dy.stride(), dx.stride()
+    fine = (dy.shape == dx.shape == (f[1], f[2], f[3] + f[4], f[5]) and sy[:3] == f[11:14] and sd[:3] == f[14:17] and sy[3] == sd[3] == 1
+            and dx.get_device() == device >= 0 and dy.dtype is dx.dtype is _TYPES.get(f[0]))
+    if not f[6] or x is None:
+        if not fine:
+            _described(f, device, (dy, 11, "dy"), (dx, 14, "dx"))
+        x = None
+    else:
+        sx = x.stride()
+        if not (fine and x.shape == dy.shape and sx[:3] == f[8:11] and sx[3] == 1 and x.get_device() == device and x.dtype is dy.dtype):
+            _described(f, device, (x, 8, "x"), (dy, 11, "dy"), (dx, 14, "dx"))
+        x = x.data_ptr()
+    if pos is None:
+        where, by_axis, by_batch = _NOWHERE
+    else:
+        where, by_axis, by_batch = _positions(f[19], f[1], f[2], pos)
+        if pos.get_device() != device:
+            _on(pos, device, "positions")
+    shape = 2 if f[4] else 1, f[5]
+    rc = lib().spb_heads_backward(desc, x, dy.data_ptr(), dx.data_ptr(), where, by_axis, by_batch, _weights(gamma, shape, f[0], device, "gamma"),
+                                  _weights(dgamma, shape, _F32, device, "dgamma"), _weights(dbeta, shape, _F32, device, "dbeta"), _workspace(workspace, workspace_bytes, device),
+                                  workspace_bytes, stream)
+    if rc:
+        _check(rc)
 
 
 def spb_encoder_heads(m, rotary, pos, norm=False, eps=1e-5):
     """pos: [axes, batch or 1, seq] int32 on the device, for the model's batch and seq, which must outlive its passes; see spb.h."""
     where, by_axis, by_batch = None, 0, 0
     if pos is not None:
-        d = spb_heads_desc()
-        d.batch, d.seq = pos.shape[1], pos.shape[2]
-        if rotary is not None:
-            d.rotary = rotary
-        where, by_axis, by_batch = _positions(d, pos)
+        where, by_axis, by_batch = _positions(rotary.axes if rotary is not None else 0, pos.shape[1], pos.shape[2], pos)
     _check(lib().spb_encoder_heads(m, C.byref(rotary) if rotary is not None else None, where, by_axis, by_batch, int(bool(norm)), eps))
 
 
@@ -425,7 +494,6 @@ def muon_config(lr, rms=0.2, momentum=0.95, nesterov=True, ns_steps=5, ns_eps=1e
 _MUON = struct.Struct("<4Q2qd4i")      # spb_muon_tensor
 assert _MUON.size == C.sizeof(spb_muon_tensor)
 _MUON_LAYOUT = "m, v and gradients are contiguous float32 tensors of the parameter's shape, which is contiguous too"
-_F32 = DTYPES["f32"]
 
 
 def _muon_tensors(tensors, pointers=True):
