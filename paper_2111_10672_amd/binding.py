@@ -417,10 +417,6 @@ def _workspace(t, size, device):
     return t.data_ptr()
 
 
-def _address(t):
-    return None if t is None else t if isinstance(t, int) else t.data_ptr()
-
-
 _NOWHERE = None, 0, 0
 
 
@@ -493,14 +489,15 @@ def muon_config(lr, rms=0.2, momentum=0.95, nesterov=True, ns_steps=5, ns_eps=1e
 
 _MUON = struct.Struct("<4Q2qd4i")      # spb_muon_tensor
 assert _MUON.size == C.sizeof(spb_muon_tensor)
-_MUON_LAYOUT = "m, v and gradients are contiguous float32 tensors of the parameter's shape, which is contiguous too"
+_MUON_LAYOUT = "m, v and gradients are contiguous float32 tensors of the parameter's shape, which is contiguous too, all on one GPU"
 
 
 def _muon_tensors(tensors, pointers=True):
-    """List of tensors given as dict(w, m, v=None, grads=[...], blocks=0, rate_scale=1.0) as C lays it out, and what keeps the arrays it points to
-    alive.  A stack [blocks, rows, cols] is its matrices' rows one after the other; any other tensor has its first dimension as rows.  Without
+    """List of tensors given as dict(w, m, v=None, grads=[...], blocks=0, rate_scale=1.0) as C lays it out, what keeps the arrays it points to
+    alive, and their GPU.  A stack [blocks, rows, cols] is its matrices' rows one after the other; any other tensor has its first dimension as rows.  Without
     pointers: shapes only."""
     stored, packed = _stored(), []
+    device = tensors[0]["w"].get_device() if tensors and pointers else 0
     held = array.array("Q", [g.data_ptr() for t in tensors for g in t["grads"]]) if pointers else None
     at = held.buffer_info()[0] if pointers else 0
     for t in tensors:
@@ -512,16 +509,16 @@ def _muon_tensors(tensors, pointers=True):
         if pointers:
             m, v, grads = t["m"], t.get("v"), t["grads"]
             for x in (m, *grads) if v is None else (m, v, *grads):
-                if stored.get(x.dtype) != _F32 or x.shape != shape or not x.is_contiguous():
+                if stored.get(x.dtype) != _F32 or x.shape != shape or not x.is_contiguous() or x.get_device() != device:
                     raise ValueError(_MUON_LAYOUT)
-            if not w.is_contiguous():
+            if not w.is_contiguous() or w.get_device() != device or device < 0:
                 raise ValueError(_MUON_LAYOUT)
             pw, pm, pv, pg, count = w.data_ptr(), m.data_ptr(), 0 if v is None else v.data_ptr(), at, len(grads)
             at += 8 * count
         dims = len(shape)
         rows = shape[0] * shape[1] if dims == 3 and blocks >= 1 and shape[0] == blocks else shape[0] if dims else 1
         packed.append(_MUON.pack(pw, pm, pv, pg, rows, w.numel() // rows if rows else 0, t.get("rate_scale", 1.0), count, code, blocks, 0))
-    return b"".join(packed), held
+    return b"".join(packed), held, device
 
 
 def spb_muon_workspace_size(tensors) -> int:
@@ -532,8 +529,8 @@ def spb_muon_workspace_size(tensors) -> int:
 
 
 def spb_muon_step(tensors, config: spb_muon_config, workspace, workspace_bytes, stream):
-    listed, _held = _muon_tensors(tensors)
-    _check(lib().spb_muon_step(listed, len(tensors), config, _address(workspace), workspace_bytes, stream))
+    listed, _held, device = _muon_tensors(tensors)
+    _check(lib().spb_muon_step(listed, len(tensors), config, _workspace(workspace, workspace_bytes, device), workspace_bytes, stream))
 
 
 def spb_aggregate_muon_workspace_size(m, blocks) -> int:

@@ -173,3 +173,25 @@ def test_tensors_side_by_side_and_gradients_of_one_place_are_taken(run):  # noqa
 for patch in (dict(), dict(m0=PLACES["w0"] + 120), dict(w1=PLACES["w0"] - 160), dict(g1=PLACES["w0"] - 160), dict(g0=PLACES["g1"]), dict(g0=PLACES["v1"] + 160)):
     _places(spb.lib(), **patch)
 """)
+
+
+# ---- tensors as Python hands them over --------------------------------------------------------------------------------
+
+def test_tensors_in_host_memory_are_refused():
+    with pytest.raises(ValueError, match="GPU"):
+        spb.spb_muon_step([_tensor((300,), 0, torch.float32, 1, 0, device="cpu")], spb.muon_config(**HYPER), None, 0, 0)
+    spb.spb_muon_step([], spb.muon_config(**HYPER), None, 0, 0)
+
+
+@pytest.mark.gpu
+def test_what_lies_elsewhere_or_is_too_small_is_refused_beside_tensors_on_the_gpu():
+    a, b = _tensor((30, 40), 1, torch.bfloat16, 2, 0), _tensor((300,), 0, torch.float32, 1, 1)
+    size = spb.spb_muon_workspace_size([a, b])
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    for tensors in ([{**a, "w": a["w"].cpu()}, b], [a, {**b, "w": b["w"].cpu()}], [{**a, "m": a["m"].cpu()}, b], [a, {**b, "v": b["v"].cpu()}],
+                    [{**a, "grads": [a["grads"][0], a["grads"][1].cpu()]}, b]):
+        with pytest.raises(ValueError, match="GPU"):
+            spb.spb_muon_step(tensors, spb.muon_config(**HYPER), ws, size, 0)
+    for workspace in (ws.cpu(), ws[:size - 1]):
+        with pytest.raises(ValueError, match="workspace"):
+            spb.spb_muon_step([a, b], spb.muon_config(**HYPER), workspace, size, 0)
