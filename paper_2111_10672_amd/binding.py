@@ -533,8 +533,15 @@ def spb_muon_step(tensors, config: spb_muon_config, workspace, workspace_bytes, 
     _check(lib().spb_muon_step(listed, len(tensors), config, _workspace(workspace, workspace_bytes, device), workspace_bytes, stream))
 
 
+def _one_per_parameter(m, *lists):
+    n = spb_param_count(m)
+    if any(len(x) != n for x in lists):
+        raise ValueError(f"lists of {sorted({len(x) for x in lists})} entries for {n} parameters")
+
+
 def spb_aggregate_muon_workspace_size(m, blocks) -> int:
     n = C.c_size_t()
+    _one_per_parameter(m, blocks)
     _check(lib().spb_aggregate_muon_workspace_size(m, (C.c_int32 * len(blocks))(*blocks), C.byref(n)))
     return n.value
 
@@ -542,9 +549,14 @@ def spb_aggregate_muon_workspace_size(m, blocks) -> int:
 def spb_aggregate_muon(m, depths, worker_grads, blocks, first, second, config: spb_muon_config, scale_lr, workspace, workspace_bytes, stream):
     """worker_grads as in spb_aggregate_update; blocks, first, second: one entry per parameter (second: None for matrices)."""
     n = len(depths)
+    if len(worker_grads) != n:
+        raise ValueError(f"gradients of {len(worker_grads)} workers, depths of {n}")
+    _one_per_parameter(m, blocks, first, second, *worker_grads)
     flat = [g for per_worker in worker_grads for g in per_worker]
+    held = workspace is None or isinstance(workspace, int)
     _check(lib().spb_aggregate_muon(m, n, (C.c_int32 * n)(*depths), _ptr_array(flat), (C.c_int32 * len(blocks))(*blocks), _ptr_array(first),
-                                    _ptr_array(second), C.byref(config), int(bool(scale_lr)), _ptr(workspace), workspace_bytes, C.c_void_p(stream)))
+                                    _ptr_array(second), C.byref(config), int(bool(scale_lr)),
+                                    workspace if held else _workspace(workspace, workspace_bytes, max(workspace.get_device(), 0)), workspace_bytes, C.c_void_p(stream)))
 
 
 def spb_set_kernel_timing(m, enable: bool):

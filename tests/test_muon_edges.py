@@ -195,3 +195,24 @@ def test_what_lies_elsewhere_or_is_too_small_is_refused_beside_tensors_on_the_gp
     for workspace in (ws.cpu(), ws[:size - 1]):
         with pytest.raises(ValueError, match="workspace"):
             spb.spb_muon_step([a, b], spb.muon_config(**HYPER), workspace, size, 0)
+
+
+def test_lists_of_the_server_step_have_an_entry_per_parameter():
+    """Shorter ones were read behind their end, on the host."""
+    import workloads as wl
+    m = spb.spb_model_create(spb.desc_from_config(wl.get_config("ragged_mlp_bf16")))
+    try:
+        n = spb.spb_param_count(m)
+        spb.spb_bind_params(m, [(i + 1) << 32 for i in range(n)])
+        blocks = [int(len(spb.spb_param_info(m, i)["shape"]) > 1) for i in range(n)]
+        size = spb.spb_aggregate_muon_workspace_size(m, blocks)
+        at = lambda k: [(k << 44) + (i << 32) for i in range(n)]
+        good = dict(depths=[4, 2], worker_grads=[at(1), at(1)], blocks=blocks, first=at(2), second=at(3), workspace=1 << 60)
+        for bad in (dict(worker_grads=[at(1)]), dict(worker_grads=[at(1), at(1)[1:]]), dict(blocks=blocks[1:]), dict(blocks=blocks + [1]), dict(first=at(2)[:-1]), dict(second=[]),
+                    dict(workspace=torch.empty(size - 1, dtype=torch.uint8)), dict(workspace=torch.empty(size, dtype=torch.uint8))):
+            with pytest.raises(ValueError):
+                spb.spb_aggregate_muon(m, **{**good, **bad}, config=spb.muon_config(**HYPER), scale_lr=True, workspace_bytes=size, stream=0)
+        with pytest.raises(ValueError):
+            spb.spb_aggregate_muon_workspace_size(m, blocks[1:])
+    finally:
+        spb.spb_model_destroy(m)
