@@ -195,6 +195,7 @@ def _ptr(t):
 def spb_model_create(desc: spb_model_desc) -> C.c_void_p:
     out = C.c_void_p()
     _check(lib().spb_model_create(C.byref(desc), C.byref(out)))
+    out.batch, out.seq = desc.batch, desc.seq      # what tensors per token are compared with
     return out
 
 
@@ -478,7 +479,11 @@ def spb_encoder_heads(m, rotary, pos, norm=False, eps=1e-5):
     """pos: [axes, batch or 1, seq] int32 on the device, for the model's batch and seq, which must outlive its passes; see spb.h."""
     where, by_axis, by_batch = None, 0, 0
     if pos is not None:
-        where, by_axis, by_batch = _positions(rotary.axes if rotary is not None else 0, pos.shape[1], pos.shape[2], pos)
+        if len(pos.shape) != 3:
+            raise ValueError(f"positions are int32 [axes, batch, seq], not {pos.dtype} {tuple(pos.shape)}")
+        # (seq 0: no encoder, which the call below says)
+        batch, seq = (m.batch, m.seq) if getattr(m, "seq", 0) else pos.shape[1:]
+        where, by_axis, by_batch = _positions(rotary.axes if rotary is not None else 0, batch, seq, pos)
     _check(lib().spb_encoder_heads(m, C.byref(rotary) if rotary is not None else None, where, by_axis, by_batch, int(bool(norm)), eps))
 
 

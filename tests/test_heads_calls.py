@@ -137,3 +137,19 @@ def test_workspaces_smaller_than_said_are_refused():
     from paper_2111_10672_amd.binding import _workspace
     _refused("bytes", lambda: _workspace(torch.empty(99, dtype=torch.uint8), 100, -1))
     assert _workspace(None, 0, 0) is None and _workspace(1 << 20, 100, 0) == 1 << 20
+
+
+def test_an_encoders_positions_are_those_of_its_tokens():
+    """They are read by every later pass: fewer than the model's tokens would be read out of range."""
+    import workloads as wl
+    cfg = wl.get_config("small_encoder_bf16")
+    b, s, rotary = cfg["batch"], cfg["seq"], spb.spb_rotary_sections([4, 4])
+    m = spb.spb_model_create(spb.desc_from_config(cfg))
+    try:
+        for shape in ((2, 1, s - 1), (2, 1, s + 1), (2, b + 1, s), (1, b, s), (2, s), (2, b, s, 1)):
+            _refused("positions", lambda: spb.spb_encoder_heads(m, rotary, torch.zeros(shape, dtype=torch.int32)))
+        _refused("positions", lambda: spb.spb_encoder_heads(m, rotary, torch.zeros(2, b, s)))
+        for shape in ((2, 1, s), (2, b, s), (3, b, s)):
+            spb.spb_encoder_heads(m, rotary, torch.zeros(shape, dtype=torch.int32))
+    finally:
+        spb.spb_model_destroy(m)
