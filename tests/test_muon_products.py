@@ -190,6 +190,35 @@ def test_settings(patch, dtype):
         check_matrices(before, _numpy(t), dtype, hyper, 0.75)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_replayed_graphs(dtype):
+    """Every way of forming the steps in one graph, replayed with the program's own work between."""
+    shapes = [(1, 20, 300), (2, 100, 300), (1, 300, 310), (8, 420, 400), (16, 600, 640)]
+    tensors = [_tensor((b * r, c), b, dtype, 2, seed=r) for b, r, c in shapes]
+    start = [(t["w"].clone(), t["m"].clone()) for t in tensors]
+    _step(tensors)                                                        # (company may change tiles, and with them the order of sums)
+    want = [(t["w"].clone(), t["m"].clone()) for t in tensors]
+    size = spb.spb_muon_workspace_size(tensors)
+    ws, side = torch.empty(size, dtype=torch.uint8, device="cuda"), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            spb.spb_muon_step(tensors, spb.muon_config(**HYPER), ws, size, side.cuda_stream)
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        for t, (w, m) in zip(tensors, start):
+            t["w"].copy_(w)
+            t["m"].copy_(m)
+        ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, (w, m) in zip(tensors, want):
+            assert torch.equal(t["w"], w) and torch.equal(t["m"], m), t["w"].shape
+
+
 # ---- what the tolerances refuse, without a GPU ------------------------------------------------------------------------
 
 @pytest.mark.parametrize("steps,most", [(1, {BF16: 0.02, F32: 1e-4}), (2, {BF16: 0.15, F32: 1e-3})])

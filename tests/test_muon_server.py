@@ -110,7 +110,6 @@ def test_server_step_against_the_oracles(name, depths, scale_lr):
         flat = lambda t: np.asarray(t).reshape(len(g), -1)
         for rows in np.split(np.arange(len(g)), blocks[n]):
             step = rate * HYPER["rms"] * math.sqrt(max(len(rows), u.shape[1]))
-            # (a matrix of the same shape in another parameter changes no bits, so its count here does not matter)
             room = step * frobenius_room(u[rows], params[n].dtype == torch.bfloat16, HYPER, blocks[n])
             room += half * np.linalg.norm(flat(want[0][n])[rows]) + 4 * U * np.linalg.norm(flat(params[n].double().numpy())[rows])
             assert np.linalg.norm(flat(w)[rows] - flat(want[0][n])[rows]) <= room, n
