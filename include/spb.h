@@ -282,7 +282,7 @@ typedef struct spb_rotary {
 typedef struct spb_heads_desc {
   int32_t dtype;               /* SPB_DTYPE_F32 or SPB_DTYPE_BF16: x, y, dy, dx, gamma, beta */
   int32_t batch, seq;          /* tokens: batch * seq, at most 2^31 - 1; either may be 0 */
-  int32_t heads_q, heads_k;    /* the first heads_q >= 1 heads take row 0 of gamma and beta, the heads_k >= 0 behind them row 1 */
+  int32_t heads_q, heads_k;    /* the first heads_q >= 1 heads take row 0 of gamma and beta, the heads_k >= 0 behind them row 1; at most 65535 in all */
   int32_t head_dim;            /* 1..SPB_MAX_HEAD_DIM */
   int32_t norm;                /* non-zero: with norm */
   float eps;                   /* > 0 with norm */
@@ -342,7 +342,9 @@ int spb_encoder_heads(spb_model* m, const spb_rotary* rotary, const int32_t* pos
  *       m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2;
  *       w = w (1 - rate weight_decay) - rate (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + adam_eps)
  * m and v are float32.  A bfloat16 parameter is rounded to nearest-even after the float32 update.  The products accumulate in float32; between them X is
- * held to 11 bits for bfloat16 parameters and to 22 bits for float32 ones. */
+ * held to 11 bits for bfloat16 parameters (X is then off by about 1e-3 of its norm after five steps, less than rounding it to bfloat16 would make it) and to 22 bits for
+ * float32 ones; matrices with a short side of at most 32 (48 for float32) go through up to 8 steps in float64.  Which kernels form a matrix's products, and with them its last bits,
+ * goes by all the matrices of a call. */
 typedef struct spb_muon_tensor {
   void* w;                     /* device, [rows, cols] dense, updated in place */
   float* m;                    /* device, the same shape: momentum, or AdamW's first moment; updated in place */

@@ -10,7 +10,8 @@
 // The elementwise half is memory-bound and one launch over a table of tensors (update_kernel); for matrices it leaves u
 // (float32) and the partial sums of |u|^2 (float64, so that neither tiny nor huge gradients leave the range) in the workspace.  24 matrices of
 // 4096 x 1024 with one worker: 279 us, 5.8 TB/s; AdamW of 23.4 million bfloat16 with four: 146 us, 5.8 TB/s.
-// The products are bound by the matrix cores where there are many tiles (24 of 1024 x 4096 x 1024: 207 us, 1.0 PFLOP/s), by launches and latency where there
+// The products are bound by the matrix cores where there are many tiles (24 of 1024 x 4096 x 1024: 207 us, 1.0 PFLOP/s; the symmetric ones
+// of 48 of 768 x 768, 0.53 PFLOP/s of useful work in 41 us, are two rounds of tiles of 128, each with a start and stores that nothing covers), by launches and latency where there
 // are few; kernels for each are below.  All matrices of one padding go through a product in one launch, whichever
 // tensors and blocks they come from, and the two symmetric products form the tiles on and below the diagonal only and
 // write each twice: a step of an r x c matrix costs r^2 c + r^3 + 2 r^2 c operations instead of 2 r^2 c + 2 r^3 + 2 r^2 c.
@@ -18,6 +19,9 @@
 // Number formats.  X, A and B are stored as float16 between the products, which accumulate in float32: at the same matrix
 // rate as bfloat16 it carries three bits more, and the step is a polynomial of a matrix of norm near 1, whose entries a fixed power of two
 // (sigma, tau) keeps in range: |X| <= 1.3 in the spectral norm throughout, so sigma |x| <= 1.3 * 2^14 and tau |b| <= 2^14.
+// For a bfloat16 parameter that leaves the orthogonalised matrix 0.9e-3 to 1.2e-3 off in the Frobenius norm (48 of 768 x 768, 24 of 4096 x 1024; up to 4e-3 where a few
+// directions stand far above the rest), where float32 in its place leaves 2e-6 to 3e-6 and rounding it to bfloat16 would leave 1.7e-3.  Added to the parameter it is not seen: that is
+// 1.66e-3 from the one in 64 bits either way, its own rounding, and 5e-4 to 7e-4 from the one with float32 in between (roundings that fall to the other side).
 // A float32 parameter would show the 2^-11 of that format: its X, A and B are stored as two float16 (value and remainder, the remainder
 // scaled by 2^11), and a product is three: value x remainder, remainder x value, their sum scaled by 2^-11, value x value.
 #include <algorithm>
@@ -972,8 +976,9 @@ __global__ __launch_bounds__(kShareThreads) void share_gram_kernel(Groups groups
 // The second and third product of a step in one launch: X' = a X + A Z with Z = b X + c A X, for a strip of 16 columns, whose products need nothing of the other
 // strips.  A wavefront has 32 rows; its part of A, the left operand of both products, goes from memory to registers and stays there, and the strip's X and Z
 // lie transposed in LDS, k contiguous.  Z takes the place of B as what is rounded to float16 in between: |Z| <= 2.9 in the spectral norm where X stays
-// below 1.3, so sigma |z| <= 2.9 * 2^14.  Bound by the load of A, 64 bytes a clock into a CU: 256 x 784 in float32 7.6 us, in bfloat16 4.6, and 13 and 7.3 with A in
-// rows, where a quarter of a wavefront's load asks for 16 lines.
+// below 1.3, so sigma |z| <= 2.9 * 2^14.  256 x 784 takes 7.9 us in float32 and 4.5 in bfloat16 on 52 CUs, and 13 and 7.3 with A in rows, where a quarter of a wavefront's
+// load asks for 16 lines.  No rate bounds it: of the 7.9 the least launch is 3, the load of A at 64 bytes a clock into a CU 1.7 and the multiplications 1.3 (in bfloat16
+// 0.9 and 0.4 of 4.5); the rest is a chain of loads, LDS round trips and three barriers that wait for one another.
 template <bool FINAL, int PLANES, int MP>
 __device__ __forceinline__ void pair_strip(const Group& g, int mat, int strip, char* lds) {
   constexpr int W = kStrip, LD = MP + 8, LF = MP + 4, STEPS = MP / 32;
@@ -1357,7 +1362,7 @@ __global__ __launch_bounds__(kThreads) void narrow_apply_kernel(NarrowGroups gro
 // themselves (rings of 96 and 128 KB); those of 128 share one with another once there are more than CUs (24 products of 1024 x 4096 x 1024: 272 us so, 345 us
 // alone on a ring of four), and have it to themselves before (136 tiles over k = 2048: 26 against 23).  One float32 product of 1024 x 1024 x 1024: tiles
 // of 64 13 us, of 128 24; 16 of them: 175 and 112.  Symmetric ones in many rounds: 19 matrices
-// of 617 x 1467, both products of a step in tiles of 64 145 us, of 128 126.  One of 256 x 256 x 784: tiles of 32 6.0 us, of 64 10.5; one bfloat16 product of 512 cubed 4.2 and 6.2, of 2048
+// of 617 x 1467, both products of a step in tiles of 64 145 us, of 128 126 (the 0.7 rests on this one shape).  One of 256 x 256 x 784: tiles of 32 6.0 us, of 64 10.5; one bfloat16 product of 512 cubed 4.2 and 6.2, of 2048
 // cubed 80 and 55, and in tiles of 128 25.  48 of 768 x 768 x 768: tiles of 128 62 us, of 256 53; their symmetric halves 44 and 53.
 double product_cost(int mode, long long tiles, int tile, int planes, int k) {
   const double steps = k / 64;
